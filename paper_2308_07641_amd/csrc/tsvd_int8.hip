@@ -1,0 +1,284 @@
+// Layers in 8-bit integers (include/tsvd_int8.h): the codes of activations, the packed weights, the entry points.
+//
+// Codes: q = rne(x 127 / a), a the largest magnitude of the token.  Bound by memory: x once, a byte for each value back; five
+// operations a value (unpacking, the magnitude's two, one fma that multiplies and rounds, its share of the byte permutes).
+#include "tsvd_int8.h"
+
+#include <algorithm>
+#include <new>
+
+#include "tsvd_scratch.h"
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
+long long round_up(long long v, long long m) { return (v + m - 1) / m * m; }
+
+// The largest over the workgroup's wavefronts.
+template <int T>
+__device__ __forceinline__ uint32_t workgroup_top(uint32_t top, uint32_t* lds) {
+    top = int8_wave_top(top);
+    if constexpr (T > 64) {
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) lds[wave] = top;
+        __syncthreads();
+        top = 0;
+#pragma unroll
+        for (int w = 0; w < T / 64; ++w) top = max(top, lds[w]);
+        __syncthreads();
+    }
+    return top;
+}
+
+// Token-major x.  T threads for a token, NV vectors of eight values each, which stay in registers between the largest magnitude and the codes; NV = 0: a loop, x
+// read twice (the second time from the caches).  T = 64: four tokens a workgroup.
+template <typename X, int T, int NV>
+__global__ void __launch_bounds__(T == 64 ? 256 : T)
+int8_quantize_rows_kernel(const X* __restrict__ x, long long ldx, long long B, int N, uint8_t* __restrict__ q, long long ldq, float* __restrict__ s) {
+    __shared__ uint32_t lds[T / 64];
+    constexpr int TOKENS = T == 64 ? 4 : 1;
+    const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, nvec = (N + 7) / 8;
+    for (long long b = (long long)blockIdx.x * TOKENS + (T == 64 ? threadIdx.x >> 6 : 0); b < B; b += (long long)gridDim.x * TOKENS) {
+        const X* row = x + b * ldx;
+        uint8_t* out = q + b * ldq;
+        uint32_t top = 0;
+        float scale, factor;
+        if constexpr (NV > 0) {
+            int8_eight<X> r[NV];
+#pragma unroll
+            for (int k = 0; k < NV; ++k) r[k] = int8_load8(row, (t + k * T) * 8, N);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) top = int8_top8(r[k], top);
+            int8_factors(workgroup_top<T>(top, lds), &scale, &factor);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (t + k * T < nvec) *reinterpret_cast<uint2*>(out + (size_t)(t + k * T) * 8) = int8_codes8(r[k], factor);
+        } else {
+            for (int v = t; v < nvec; v += T) top = int8_top8(int8_load8(row, v * 8, N), top);
+            int8_factors(workgroup_top<T>(top, lds), &scale, &factor);
+            for (int v = t; v < nvec; v += T) *reinterpret_cast<uint2*>(out + (size_t)v * 8) = int8_codes8(int8_load8(row, v * 8, N), factor);
+        }
+        if (t == 0) s[b] = scale;
+    }
+}
+
+// Feature-major x [N][B]: a workgroup takes 8 TV tokens.  A thread loads eight tokens of a row of x at a time; the largest magnitudes of the tokens meet in
+// LDS, then x is read again (from the caches), four rows a thread, and the codes pass through LDS so that a token's bytes leave side by side.
+template <typename X, int TV>
+__global__ void __launch_bounds__(256)
+int8_quantize_columns_kernel(const X* __restrict__ x, long long ldx, long long B, int N, uint8_t* __restrict__ q, long long ldq, float* __restrict__ s) {
+    constexpr int ROWS = 256 / TV, STEP = 4 * ROWS, PITCH = STEP + 16, TOKENS = 8 * TV;      // rows of threads; features a pass
+    __shared__ uint32_t tops[TOKENS];
+    __shared__ __align__(16) uint8_t tile[TOKENS * PITCH];
+    const int v = threadIdx.x % TV, r = threadIdx.x / TV;
+    const long long b0 = (long long)blockIdx.x * TOKENS;
+    const int tokens = (int)min((long long)TOKENS, B - b0);
+    if (threadIdx.x < TOKENS) tops[threadIdx.x] = 0;
+    __syncthreads();
+    uint32_t top[8] = {};
+    for (int n = r; n < N; n += ROWS) {
+        const int8_eight<X> e = int8_load8(x + (size_t)n * ldx + b0, 8 * v, tokens);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top[k] = max(top[k], __float_as_uint(e.get(k)) & 0x7FFFFFFFu);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) atomicMax(&tops[8 * v + k], top[k]);
+    __syncthreads();
+    float factor[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        float scale;
+        int8_factors(tops[8 * v + k], &scale, &factor[k]);
+        if (r == 0 && 8 * v + k < tokens) s[b0 + 8 * v + k] = scale;
+    }
+    for (int n0 = 0; n0 < N; n0 += STEP) {
+        const int n = n0 + 4 * r;
+        uint32_t c[4][8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            int8_eight<X> e;
+            e.zero();
+            if (n + j < N) e = int8_load8(x + (size_t)(n + j) * ldx + b0, 8 * v, tokens);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c[j][k] = int8_code(e.get(k), factor[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) *reinterpret_cast<uint32_t*>(&tile[(8 * v + k) * PITCH + 4 * r]) = int8_pack4(c[0][k], c[1][k], c[2][k], c[3][k]);
+        __syncthreads();
+        const int pieces = min(STEP, (N - n0 + 15) / 16 * 16) / 16;
+        for (int i = threadIdx.x; i < tokens * pieces; i += 256) {
+            const int b = i / pieces, at = 16 * (i - b * pieces);
+            *reinterpret_cast<u32x4*>(q + (b0 + b) * ldq + n0 + at) = *reinterpret_cast<const u32x4*>(&tile[b * PITCH + at]);
+        }
+        __syncthreads();
+    }
+}
+
+// Codes [M][ldw] -> tiles (tsvd_int8.h): a thread makes the 16 bytes of one lane.
+__global__ void __launch_bounds__(256)
+int8_pack_kernel(const uint8_t* __restrict__ w, long long ldw, long long M, int N, int nkt, long long pieces, uint8_t* __restrict__ tiles) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (long long)gridDim.x * 256) {
+        const long long tile = i >> 6, strip = tile / nkt;
+        const int l = (int)i & 63, k = (int)(tile - strip * nkt) * 64 + (l >> 4) * 16;
+        const long long row = strip * 16 + (l & 15);
+        uint32_t d[4] = {};
+        if (row < M) {
+            const uint8_t* src = w + row * ldw;
+            if (k + 16 <= N) {
+                typedef u32x4 u32x4_at __attribute__((aligned(1)));
+                const u32x4 v = *reinterpret_cast<const u32x4_at*>(src + k);
+                d[0] = v[0], d[1] = v[1], d[2] = v[2], d[3] = v[3];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (k + e < N) d[e >> 2] |= (uint32_t)src[k + e] << (8 * (e & 3));
+            }
+        }
+        *reinterpret_cast<u32x4*>(tiles + i * 16) = u32x4{d[0], d[1], d[2], d[3]};
+    }
+}
+__global__ void __launch_bounds__(256)
+int8_pack_scales_kernel(const float* __restrict__ t, long long M, long long rows, float* __restrict__ out) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows; i += (long long)gridDim.x * 256) out[i] = i < M ? t[i] : 0.f;
+}
+
+unsigned grid_of(long long blocks) { return (unsigned)std::min<long long>(blocks, 1 << 20); }
+
+template <typename X>
+hipError_t quantize(const X* x, bool token_major, long long B, int N, long long ldx, uint8_t* q, long long ldq, float* s, hipStream_t stream) {
+    if (token_major) {
+#define ROWS(T, NV) hipLaunchKernelGGL((int8_quantize_rows_kernel<X, T, NV>), dim3(grid_of(T == 64 ? (B + 3) / 4 : B)), dim3(T == 64 ? 256 : T), 0, stream, x, ldx, B, N, q, ldq, s)
+        if (N <= 512) ROWS(64, 1);
+        else if (N <= 1024) ROWS(64, 2);
+        else if (N <= 2048) ROWS(64, 4);
+        else if (N <= 4096) ROWS(256, 2);
+        else if (N <= 8192) ROWS(256, 4);
+        else if (N <= 16384) ROWS(256, 8);
+        else ROWS(1024, 0);
+#undef ROWS
+    } else {
+        hipLaunchKernelGGL((int8_quantize_columns_kernel<X, 4>), dim3((unsigned)((B + 31) / 32)), dim3(256), 0, stream, x, ldx, B, N, q, ldq, s);
+    }
+    return hipGetLastError();
+}
+hipError_t quantize(const void* x, tsvd_dtype x_dtype, bool token_major, long long B, int N, long long ldx, int8_t* codes, long long ldq, float* s, hipStream_t stream) {
+    uint8_t* q = reinterpret_cast<uint8_t*>(codes);
+    return x_dtype == TSVD_BF16 ? quantize(static_cast<const uint16_t*>(x), token_major, B, N, ldx, q, ldq, s, stream)
+                                : quantize(static_cast<const float*>(x), token_major, B, N, ldx, q, ldq, s, stream);
+}
+
+bool bad_codes(const void* codes, int64_t ldq, int64_t N) { return !codes || (reinterpret_cast<uintptr_t>(codes) & 15u) || ldq < N || ldq % 16 != 0; }
+bool bad_dtype(int t) { return t != TSVD_F32 && t != TSVD_BF16; }
+bool bad_layout(int l) { return l != TSVD_FEATURE_MAJOR && l != TSVD_TOKEN_MAJOR; }
+
+// One token is a contiguous vector in either layout, whatever its stride means: as one row.
+bool one_row(tsvd_layout layout, int64_t B, int64_t ldx) { return layout == TSVD_TOKEN_MAJOR || (B == 1 && ldx == 1); }
+
+size_t codes_bytes(const tsvd_int8_handle* h, int64_t B) { return round256((size_t)B * tsvd_int8_row_bytes(h->N)); }
+
+}  // namespace
+
+extern "C" size_t tsvd_int8_row_bytes(int64_t N) { return N <= 0 || N > TSVD_INT8_MAX_N ? 0 : (size_t)round_up(N, 128); }
+
+extern "C" tsvd_status tsvd_int8_quantize(const void* x_dev, tsvd_dtype x_dtype, tsvd_layout x_layout, int64_t B, int64_t N, int64_t ldx,
+                                          int8_t* codes_dev, int64_t ldq, float* scales_dev, void* stream) {
+    if (!x_dev || !scales_dev || B < 1 || N < 1 || bad_dtype(x_dtype) || bad_layout(x_layout)) return TSVD_EINVAL;
+    if (ldx < (x_layout == TSVD_TOKEN_MAJOR ? N : B) || bad_codes(codes_dev, ldq, N)) return TSVD_EINVAL;
+    if (N > TSVD_INT8_MAX_N || B > TSVD_INT8_MAX_B) return TSVD_EUNSUPPORTED;
+    const bool rows = one_row(x_layout, B, ldx);
+    return quantize(x_dev, x_dtype, rows, B, (int)N, x_layout == TSVD_TOKEN_MAJOR ? ldx : rows ? N : ldx, codes_dev, ldq, scales_dev,
+                    static_cast<hipStream_t>(stream)) == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
+}
+
+extern "C" size_t tsvd_int8_packed_bytes(int64_t M, int64_t N) {
+    if (M < 1 || N < 1 || N > TSVD_INT8_MAX_N || M > TSVD_INT8_MAX_M) return 0;
+    const size_t strips = (size_t)(M + 15) / 16;
+    return round256(strips * 64) + strips * (size_t)(round_up(N, 128) / 64) * 1024;
+}
+
+extern "C" tsvd_status tsvd_int8_pack(const int8_t* w_dev, int64_t ldw, const float* t_dev, int64_t M, int64_t N, void* dev_buf, size_t dev_buf_bytes,
+                                      void* stream, tsvd_int8_handle** out) {
+    if (!w_dev || !t_dev || !out || M < 1 || N < 1 || ldw < N) return TSVD_EINVAL;
+    if (N > TSVD_INT8_MAX_N || M > TSVD_INT8_MAX_M) return TSVD_EUNSUPPORTED;
+    const size_t bytes = tsvd_int8_packed_bytes(M, N);
+    if (dev_buf ? dev_buf_bytes < bytes || (reinterpret_cast<uintptr_t>(dev_buf) & 255u) : dev_buf_bytes != 0) return TSVD_EINVAL;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    int device = 0, cus = 0;
+    if (hipStreamIsCapturing(s, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone || hipGetDevice(&device) != hipSuccess ||
+        hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) {
+        (void)hipGetLastError();
+        return TSVD_EDEVICE;
+    }
+    tsvd_int8_handle* h = new (std::nothrow) tsvd_int8_handle();
+    if (!h) return TSVD_ENOMEM;
+    h->device = device;
+    h->cu_count = cus;
+    h->M = M, h->N = N, h->strips = (M + 15) / 16;
+    h->nkt = (int)(round_up(N, 128) / 64);
+    h->blob = static_cast<uint8_t*>(dev_buf);
+    if (!dev_buf) {
+        void* p = nullptr;
+        if (tsvd_device_malloc(&p, bytes) != hipSuccess) {
+            (void)hipGetLastError();
+            delete h;
+            return TSVD_EDEVICE;
+        }
+        h->blob = static_cast<uint8_t*>(p);
+        h->owns_blob = true;
+    }
+    const long long pieces = h->strips * h->nkt * 64;
+    hipLaunchKernelGGL(int8_pack_scales_kernel, dim3(grid_of((h->strips * 16 + 255) / 256)), dim3(256), 0, s, t_dev, (long long)M, h->strips * 16, reinterpret_cast<float*>(h->blob));
+    hipLaunchKernelGGL(int8_pack_kernel, dim3(grid_of((pieces + 255) / 256)), dim3(256), 0, s, reinterpret_cast<const uint8_t*>(w_dev), (long long)ldw, (long long)M, (int)N,
+                       h->nkt, pieces, const_cast<uint8_t*>(h->tiles()));
+    if (hipGetLastError() != hipSuccess || hipStreamSynchronize(s) != hipSuccess) {
+        (void)hipGetLastError();
+        tsvd_int8_free(h);
+        return TSVD_EDEVICE;
+    }
+    *out = h;
+    return TSVD_OK;
+}
+
+extern "C" tsvd_status tsvd_int8_info(const tsvd_int8_handle* h, int64_t* M, int64_t* N) {
+    if (!h) return TSVD_EINVAL;
+    if (M) *M = h->M;
+    if (N) *N = h->N;
+    return TSVD_OK;
+}
+
+extern "C" void tsvd_int8_free(tsvd_int8_handle* h) {
+    if (!h) return;
+    if (h->owns_blob && h->blob) (void)hipFree(h->blob);
+    delete h;
+}
+
+extern "C" tsvd_status tsvd_int8_product(const tsvd_int8_handle* h, const int8_t* codes_dev, int64_t ldq, const float* scales_dev, int64_t B,
+                                         const float* bias_dev, void* y_dev, tsvd_dtype y_dtype, tsvd_layout y_layout, int64_t ldy, void* stream) {
+    if (!h || !scales_dev || !y_dev || B < 1 || bad_dtype(y_dtype) || bad_layout(y_layout)) return TSVD_EINVAL;
+    if (bad_codes(codes_dev, ldq, h->N) || ldy < (y_layout == TSVD_TOKEN_MAJOR ? h->M : B)) return TSVD_EINVAL;
+    if (B > TSVD_INT8_MAX_B) return TSVD_EUNSUPPORTED;
+    const tsvd_int8_problem p = {h, codes_dev, ldq, scales_dev, B, bias_dev, y_dev, y_dtype == TSVD_BF16, y_layout == TSVD_TOKEN_MAJOR, ldy};
+    return tsvd_int8_gemm(p, static_cast<hipStream_t>(stream)) == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
+}
+
+extern "C" size_t tsvd_int8_workspace_bytes(const tsvd_int8_handle* h, int64_t B, tsvd_dtype x_dtype, tsvd_layout x_layout) {
+    if (!h || B < 1 || B > TSVD_INT8_MAX_B || bad_dtype(x_dtype) || bad_layout(x_layout)) return 0;
+    return codes_bytes(h, B) + round256((size_t)B * 4);
+}
+
+extern "C" tsvd_status tsvd_int8_forward(const tsvd_int8_handle* h, const void* x_dev, tsvd_dtype x_dtype, tsvd_layout x_layout, int64_t B, int64_t ldx,
+                                         const float* bias_dev, void* y_dev, tsvd_dtype y_dtype, tsvd_layout y_layout, int64_t ldy, void* workspace,
+                                         size_t workspace_bytes, void* stream) {
+    if (!h || !x_dev || !y_dev || B < 1 || bad_dtype(x_dtype) || bad_layout(x_layout) || bad_dtype(y_dtype) || bad_layout(y_layout)) return TSVD_EINVAL;
+    if (ldx < (x_layout == TSVD_TOKEN_MAJOR ? h->N : B) || ldy < (y_layout == TSVD_TOKEN_MAJOR ? h->M : B)) return TSVD_EINVAL;
+    if (B > TSVD_INT8_MAX_B) return TSVD_EUNSUPPORTED;
+    if (!workspace || workspace_bytes < tsvd_int8_workspace_bytes(h, B, x_dtype, x_layout) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return TSVD_EINVAL;
+    int8_t* codes = static_cast<int8_t*>(workspace);
+    float* scales = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + codes_bytes(h, B));
+    const int64_t ldq = (int64_t)tsvd_int8_row_bytes(h->N);
+    const tsvd_status st = tsvd_int8_quantize(x_dev, x_dtype, x_layout, B, h->N, ldx, codes, ldq, scales, stream);
+    return st != TSVD_OK ? st : tsvd_int8_product(h, codes, ldq, scales, B, bias_dev, y_dev, y_dtype, y_layout, ldy, stream);
+}

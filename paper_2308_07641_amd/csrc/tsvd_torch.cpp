@@ -8,6 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 
 #include <algorithm>
 #include <cstdint>
@@ -15,6 +16,8 @@
 
 #include "../../include/tsvd.h"
 #include "../../include/tsvd_conv.h"
+#include "../../include/tsvd_int8.h"
+#include "../../include/tsvd_norm.h"
 
 namespace {
 
@@ -272,6 +275,242 @@ PyObject* py_conv2d(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- layers in 8-bit integers and norms: the device of x is made the current one, and everything has to live there
+void same_device(const at::Tensor& t, const at::Tensor& x, const char* text) {
+    if (t.device() != x.device()) raise(PyExc_ValueError, text);
+}
+const tsvd_int8_handle* int8_handle_of(const handle_view& h) { return reinterpret_cast<const tsvd_int8_handle*>(h.ptr); }
+// Results and workspaces made here belong to torch's current stream: work on another one needs the caller's own.
+void need_own(PyObject* given, PyObject* stream, const char* text) {
+    if (given == Py_None && stream != Py_None) raise(PyExc_ValueError, text);
+}
+const float* floats_of(PyObject* o, int64_t n, const at::Tensor& x, const char* text) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor_of(o, "bias, gamma, beta and scales");
+    if (t.scalar_type() != at::kFloat || t.dim() != 1 || t.size(0) != n || !t.is_cuda() || !t.is_contiguous() || t.device() != x.device()) raise(PyExc_ValueError, text);
+    return static_cast<const float*>(t.data_ptr());
+}
+workspace_view scratch_of(PyObject* ws, size_t need, const at::Tensor& x, at::Tensor* made) {
+    if (ws == Py_None) {
+        if (need == 0) return {nullptr, 0};
+        *made = at::empty({(int64_t)need}, x.options().dtype(at::kByte));
+        return {made->data_ptr(), need};
+    }
+    const at::Tensor& w = tensor_of(ws, "workspace");
+    if (!w.is_cuda() || w.device() != x.device() || !w.is_contiguous()) raise(PyExc_ValueError, "workspace must be a contiguous GPU tensor on x's device");
+    return {w.data_ptr(), (size_t)w.numel() * w.element_size()};
+}
+// Codes [B, N] with a pitch of ldq bytes.
+struct codes_view {
+    int8_t* ptr;
+    int64_t B, N, ldq;
+};
+codes_view codes_of(PyObject* o) {
+    const at::Tensor& c = tensor_of(o, "codes");
+    if (!c.is_cuda() || c.scalar_type() != at::kChar || c.dim() != 2 || (c.size(1) > 1 && c.stride(1) != 1))
+        raise(PyExc_ValueError, "codes must be an int8 GPU tensor [B,N] with unit inner stride");
+    const int64_t rows = c.size(0), n = c.size(1);
+    return {static_cast<int8_t*>(c.data_ptr()), rows, n, rows > 1 ? c.stride(0) : (n + 15) / 16 * 16};
+}
+PyObject* new_codes(int64_t B, int64_t N, const at::Tensor& x) {
+    return THPVariable_Wrap(at::empty({B, (int64_t)tsvd_int8_row_bytes(N)}, x.options().dtype(at::kChar)).slice(1, 0, N));
+}
+PyObject* codes_and_scales(y_ref& codes, y_ref& scales) {
+    PyObject* r = PyTuple_Pack(2, codes.p, scales.p);
+    if (!r) throw failed();
+    return r;
+}
+void check_codes(const codes_view& c, int64_t B, int64_t N, const char* text) {
+    if (c.B != B || c.N != N) raise(PyExc_ValueError, text);
+}
+// A single row of codes: only what its 16-byte pieces need is known to be there.
+void check_single_row(PyObject* o) {
+    const at::Tensor& c = THPVariable_Unpack(o);
+    const int64_t left = (int64_t)c.storage().nbytes() - c.storage_offset();
+    if (c.size(0) == 1 && left < (c.size(1) + 15) / 16 * 16) raise(PyExc_ValueError, "codes: a row needs room up to the next multiple of 16 bytes");
+}
+
+// int8_quantize(x, x_layout, codes, scales, stream)
+PyObject* py_int8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        need_args(n, 5, "int8_quantize");
+        const at::Tensor& x = tensor_of(a[0], "x");
+        if (!x.is_cuda() || x.dim() != 2 || x.stride(1) != 1) raise(PyExc_ValueError, "x must be a 2-d GPU tensor with unit inner stride");
+        const c10::DeviceGuard device(x.device());
+        const tsvd_layout xl = (tsvd_layout)integer(a[1]);
+        const bool xt = xl == TSVD_TOKEN_MAJOR;
+        const int64_t B = x.size(xt ? 0 : 1), N = x.size(xt ? 1 : 0), ldx = row_pitch(x);
+        const tsvd_dtype xd = dtype_code(x);
+        need_own(a[2], a[4], "work on a stream of your own needs codes and scales of your own");
+        need_own(a[3], a[4], "work on a stream of your own needs codes and scales of your own");
+        y_ref codes{a[2] == Py_None ? new_codes(B, N, x) : Py_NewRef(a[2])}, scales{a[3] == Py_None ? THPVariable_Wrap(at::empty({B}, x.options().dtype(at::kFloat))) : Py_NewRef(a[3])};
+        if (!codes.p || !scales.p) throw failed();
+        const codes_view c = codes_of(codes.p);
+        check_codes(c, B, N, "codes must be [B,N]");
+        check_single_row(codes.p);
+        same_device(THPVariable_Unpack(codes.p), x, "codes must live on x's device");
+        float* s = const_cast<float*>(floats_of(scales.p, B, x, "scales must be a contiguous float32 GPU tensor [B] on x's device"));
+        void* stream = stream_of(a[4], x);
+        const void* xp = x.data_ptr();
+        tsvd_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = tsvd_int8_quantize(xp, xd, xl, B, N, ldx, c.ptr, c.ldq, s, stream);
+        Py_END_ALLOW_THREADS
+        check(st, "tsvd_int8_quantize");
+        return codes_and_scales(codes, scales);
+    });
+}
+
+// int8_layer(h, x, x_layout, bias, y, y_dtype, y_layout, workspace, stream)
+PyObject* py_int8_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        need_args(n, 9, "int8_layer");
+        const handle_view h = handle_of(a[0]);
+        const at::Tensor& x = tensor_of(a[1], "x");
+        if (!x.is_cuda() || x.dim() != 2 || x.stride(1) != 1) raise(PyExc_ValueError, "x must be a 2-d GPU tensor with unit inner stride");
+        const c10::DeviceGuard device(x.device());
+        const tsvd_layout xl = (tsvd_layout)integer(a[2]), yl = (tsvd_layout)integer(a[6]);
+        const int64_t yd = integer(a[5]);
+        const bool xt = xl == TSVD_TOKEN_MAJOR, ytm = yl == TSVD_TOKEN_MAJOR;
+        const int64_t B = x.size(xt ? 0 : 1), ldx = row_pitch(x);
+        if (x.size(xt ? 1 : 0) != h.N) raise(PyExc_ValueError, "x does not have N features");
+        const tsvd_dtype xd = dtype_code(x);
+        need_own(a[4], a[8], "work on a stream of your own needs a y of your own");
+        y_ref y{result_of(a[4], ytm ? B : h.M, ytm ? h.M : B, yd == TSVD_BF16 ? at::kBFloat16 : at::kFloat, x,
+                          "y must be a GPU tensor of the requested type and layout with unit inner stride")};
+        if (!y.p) throw failed();
+        const at::Tensor& yt = THPVariable_Unpack(y.p);
+        same_device(yt, x, "y must live on x's device");
+        const float* bias = floats_of(a[3], h.M, x, "bias must be a contiguous float32 GPU tensor [M] on x's device");
+        const size_t need = tsvd_int8_workspace_bytes(int8_handle_of(h), B, xd, xl);
+        if (need) need_own(a[7], a[8], "work on a stream of your own needs a workspace of your own");
+        at::Tensor made;
+        const workspace_view ws = scratch_of(a[7], need, x, &made);
+        void* stream = stream_of(a[8], x);
+        const void* xp = x.data_ptr();
+        void* yp = yt.data_ptr();
+        const int64_t ldy = row_pitch(yt);
+        tsvd_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = tsvd_int8_forward(int8_handle_of(h), xp, xd, xl, B, ldx, bias, yp, (tsvd_dtype)yd, yl, ldy, ws.ptr, ws.bytes, stream);
+        Py_END_ALLOW_THREADS
+        check(st, "tsvd_int8_forward");
+        return y.release();
+    });
+}
+
+// int8_product(h, codes, scales, bias, y, y_dtype, y_layout, stream)
+PyObject* py_int8_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        need_args(n, 8, "int8_product");
+        const handle_view h = handle_of(a[0]);
+        const codes_view c = codes_of(a[1]);
+        const at::Tensor& q = THPVariable_Unpack(a[1]);
+        const c10::DeviceGuard device(q.device());
+        if (c.N != h.N) raise(PyExc_ValueError, "codes do not have N features");
+        check_single_row(a[1]);
+        const tsvd_layout yl = (tsvd_layout)integer(a[6]);
+        const int64_t yd = integer(a[5]);
+        const bool ytm = yl == TSVD_TOKEN_MAJOR;
+        need_own(a[4], a[7], "work on a stream of your own needs a y of your own");
+        y_ref y{result_of(a[4], ytm ? c.B : h.M, ytm ? h.M : c.B, yd == TSVD_BF16 ? at::kBFloat16 : at::kFloat, q,
+                          "y must be a GPU tensor of the requested type and layout with unit inner stride")};
+        if (!y.p) throw failed();
+        const at::Tensor& yt = THPVariable_Unpack(y.p);
+        same_device(yt, q, "y must live on the codes' device");
+        const float* bias = floats_of(a[3], h.M, q, "bias must be a contiguous float32 GPU tensor [M] on the codes' device");
+        const float* scales = floats_of(a[2], c.B, q, "scales must be a contiguous float32 GPU tensor [B] on the codes' device");
+        void* stream = stream_of(a[7], q);
+        void* yp = yt.data_ptr();
+        const int64_t ldy = row_pitch(yt);
+        tsvd_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = tsvd_int8_product(int8_handle_of(h), c.ptr, c.ldq, scales, c.B, bias, yp, (tsvd_dtype)yd, yl, ldy, stream);
+        Py_END_ALLOW_THREADS
+        check(st, "tsvd_int8_product");
+        return y.release();
+    });
+}
+
+// group_norm(x, groups, gamma, beta, eps, act, y, y_dtype, y_layout, workspace, stream): x [rows, C], [images, positions, C] or [images, H, W, C];
+// group_norm_int8(x, groups, gamma, beta, eps, act, codes, scales, workspace, stream)
+template <bool CODES>
+PyObject* py_group_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        need_args(n, CODES ? 10 : 11, CODES ? "group_norm_int8" : "group_norm");
+        PyObject *const workspace = a[CODES ? 8 : 9], *const stream_arg = a[CODES ? 9 : 10];
+        const at::Tensor& x = tensor_of(a[0], "x");
+        static const char* const text = "x must be a GPU tensor [rows,C], [images,positions,C] or [images,H,W,C] with unit inner stride and one pitch from a position to the next";
+        const int64_t d = x.dim();
+        if (!x.is_cuda() || d < 2 || d > 4 || x.numel() == 0 || (x.size(d - 1) > 1 && x.stride(d - 1) != 1)) raise(PyExc_ValueError, text);
+        const c10::DeviceGuard device(x.device());
+        const int64_t C = x.size(d - 1), images = x.size(0), P = x.numel() / (images * C);
+        int64_t ldx = 0, before = 1;                                   // the pitch that every dimension longer than one has to agree with
+        for (int64_t k = d - 2; k >= 0; --k) {
+            if (x.size(k) > 1) {
+                if (ldx == 0 && x.stride(k) % before == 0) ldx = x.stride(k) / before;
+                if (x.stride(k) != ldx * before) raise(PyExc_ValueError, text);
+            }
+            before *= x.size(k);
+        }
+        if (ldx == 0) ldx = C;
+        const tsvd_dtype xd = dtype_code(x);
+        const int64_t groups = integer(a[1]);
+        const float *gamma = floats_of(a[2], C, x, "gamma must be a contiguous float32 GPU tensor [C] on x's device"),
+                    *beta = floats_of(a[3], C, x, "beta must be a contiguous float32 GPU tensor [C] on x's device");
+        const double eps = PyFloat_AsDouble(a[4]);
+        if (eps == -1.0 && PyErr_Occurred()) throw failed();
+        const tsvd_activation act = (tsvd_activation)integer(a[5]);
+        const size_t need = tsvd_group_norm_workspace_bytes(images, P, C, groups);
+        if (need) need_own(workspace, stream_arg, "work on a stream of your own needs a workspace of your own");
+        need_own(a[6], stream_arg, "work on a stream of your own needs a result of your own");
+        const void* xp = x.data_ptr();
+        tsvd_status st;
+        at::Tensor made;
+        if constexpr (CODES) {
+            need_own(a[7], stream_arg, "work on a stream of your own needs a result of your own");
+            y_ref codes{a[6] == Py_None ? new_codes(images * P, C, x) : Py_NewRef(a[6])};
+            y_ref scales{a[7] == Py_None ? THPVariable_Wrap(at::empty({images * P}, x.options().dtype(at::kFloat))) : Py_NewRef(a[7])};
+            if (!codes.p || !scales.p) throw failed();
+            const codes_view c = codes_of(codes.p);
+            check_codes(c, images * P, C, "codes must be [images * positions,C]");
+            check_single_row(codes.p);
+            same_device(THPVariable_Unpack(codes.p), x, "codes must live on x's device");
+            float* s = const_cast<float*>(floats_of(scales.p, images * P, x, "scales must be a contiguous float32 GPU tensor [images * positions] on x's device"));
+            const workspace_view ws = scratch_of(workspace, need, x, &made);
+            void* stream = stream_of(stream_arg, x);
+            Py_BEGIN_ALLOW_THREADS
+            st = tsvd_group_norm_int8(xp, xd, images, P, C, ldx, groups, gamma, beta, (float)eps, act, c.ptr, c.ldq, s, ws.ptr, ws.bytes, stream);
+            Py_END_ALLOW_THREADS
+            check(st, "tsvd_group_norm_int8");
+            return codes_and_scales(codes, scales);
+        } else {
+            const int64_t yd = integer(a[7]);
+            const tsvd_layout yl = (tsvd_layout)integer(a[8]);
+            const bool ytm = yl == TSVD_TOKEN_MAJOR;
+            const at::ScalarType dt = yd == TSVD_BF16 ? at::kBFloat16 : at::kFloat;
+            std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+            if (!ytm) {
+                shape.pop_back();
+                shape.insert(shape.begin(), C);
+            }
+            y_ref y{a[6] == Py_None ? THPVariable_Wrap(at::empty(shape, x.options().dtype(dt))) : Py_NewRef(a[6])};
+            if (!y.p) throw failed();
+            const at::Tensor& yt = tensor_of(y.p, "y");
+            if (!yt.is_cuda() || yt.scalar_type() != dt || yt.sizes() != at::IntArrayRef(shape) || !yt.is_contiguous() || yt.device() != x.device())
+                raise(PyExc_ValueError, "y must be a contiguous GPU tensor of the requested type on x's device: x's shape, or with the channels first (feature-major)");
+            const workspace_view ws = scratch_of(workspace, need, x, &made);
+            void* stream = stream_of(stream_arg, x);
+            void* yp = yt.data_ptr();
+            Py_BEGIN_ALLOW_THREADS
+            st = tsvd_group_norm(xp, xd, images, P, C, ldx, groups, gamma, beta, (float)eps, act, yp, (tsvd_dtype)yd, yl, ytm ? C : images * P, ws.ptr, ws.bytes, stream);
+            Py_END_ALLOW_THREADS
+            check(st, "tsvd_group_norm");
+            return y.release();
+        }
+    });
+}
+
 // setup(error class, raw stream lookup)
 PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
@@ -289,6 +528,11 @@ PyMethodDef methods[] = {
     {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_forward)), METH_FASTCALL, nullptr},
     {"layer", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_layer)), METH_FASTCALL, nullptr},
     {"conv2d", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_conv2d)), METH_FASTCALL, nullptr},
+    {"int8_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_int8_quantize)), METH_FASTCALL, nullptr},
+    {"int8_layer", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_int8_layer)), METH_FASTCALL, nullptr},
+    {"int8_product", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_int8_product)), METH_FASTCALL, nullptr},
+    {"group_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_group_norm<false>)), METH_FASTCALL, nullptr},
+    {"group_norm_int8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_group_norm<true>)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tsvd_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

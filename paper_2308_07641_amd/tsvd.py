@@ -14,6 +14,7 @@ TSVD_F32 = 0
 TSVD_BF16 = 1
 TSVD_FEATURE_MAJOR = 0
 TSVD_TOKEN_MAJOR = 1
+TSVD_ACT_NONE, TSVD_ACT_RELU, TSVD_ACT_SILU, TSVD_ACT_GELU = 0, 1, 2, 3
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libtsvd.so")
@@ -66,6 +67,20 @@ _PROTOTYPES = {
     "tsvd_transition_q": (ctypes.c_int, [_vp, _i64, _i64, ctypes.c_double, ctypes.c_double, _i64, _i64, _vp, _vp, _vp, _pi64, _vp, _vp]),
     "tsvd_conv2d_workspace_bytes": (_sz, [_vp, _vp, _i64, _i64, _i64]),
     "tsvd_conv2d_forward": (ctypes.c_int, [_vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, ctypes.c_int, _vp, _sz, _vp]),
+    "tsvd_int8_row_bytes": (_sz, [_i64]),
+    "tsvd_int8_quantize": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, _i64, _i64, _i64, _vp, _i64, _vp, _vp]),
+    "tsvd_int8_packed_bytes": (_sz, [_i64, _i64]),
+    "tsvd_int8_pack": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i64, _vp, _sz, _vp, ctypes.POINTER(_vp)]),
+    "tsvd_int8_info": (ctypes.c_int, [_vp, _pi64, _pi64]),
+    "tsvd_int8_free": (None, [_vp]),
+    "tsvd_int8_product": (ctypes.c_int, [_vp, _vp, _i64, _vp, _i64, _vp, _vp, ctypes.c_int, ctypes.c_int, _i64, _vp]),
+    "tsvd_int8_workspace_bytes": (_sz, [_vp, _i64, ctypes.c_int, ctypes.c_int]),
+    "tsvd_int8_forward": (ctypes.c_int, [_vp, _vp, ctypes.c_int, ctypes.c_int, _i64, _i64, _vp, _vp, ctypes.c_int, ctypes.c_int, _i64, _vp, _sz, _vp]),
+    "tsvd_group_norm_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
+    "tsvd_group_norm": (ctypes.c_int, [_vp, ctypes.c_int, _i64, _i64, _i64, _i64, _i64, _vp, _vp, ctypes.c_float, ctypes.c_int, _vp, ctypes.c_int,
+                                       ctypes.c_int, _i64, _vp, _sz, _vp]),
+    "tsvd_group_norm_int8": (ctypes.c_int, [_vp, ctypes.c_int, _i64, _i64, _i64, _i64, _i64, _vp, _vp, ctypes.c_float, ctypes.c_int, _vp, _i64, _vp,
+                                            _vp, _sz, _vp]),
     "tsvd_free": (None, [_vp]),
     "tsvd_strerror": (ctypes.c_char_p, [ctypes.c_int]),
 }
@@ -449,6 +464,109 @@ def tsvd_conv2d_forward(h: Handle, form: int, c_in: int, c_out: int, k1: int, k2
     """y [C_out, images, Ho, Wo] = conv2d(x [C_in, images, H, W] bf16) with the kernel in ternary-SVD form `form`
     (groups > 1: form 0 with per-group factors, see include/tsvd_conv.h)."""
     return (_binding or _load_binding()).conv2d(h, form, c_in, c_out, k1, k2, x, stride, pad, dil, bias, y_dtype, stream, groups)
+
+
+# ---- layers in 8-bit integers (include/tsvd_int8.h)
+class Int8Handle:
+    """Owner of a tsvd_int8_handle*; free with tsvd_int8_free (also freed on garbage collection)."""
+
+    def __init__(self, ptr: int, M: int, N: int, keepalive=None):
+        self.ptr = ptr
+        self.M, self.N = M, N
+        self._keepalive = keepalive     # caller-provided device buffer, if any
+
+    def __del__(self):
+        try:
+            tsvd_int8_free(self)
+        except Exception:
+            pass
+
+
+def tsvd_int8_row_bytes(N: int) -> int:
+    """The pitch of rows of N codes that suits the products."""
+    return int(load_library().tsvd_int8_row_bytes(N))
+
+
+def tsvd_int8_packed_bytes(M: int, N: int) -> int:
+    return int(load_library().tsvd_int8_packed_bytes(M, N))
+
+
+def tsvd_int8_quantize(x, x_layout=TSVD_TOKEN_MAJOR, codes=None, scales=None, stream=None):
+    """(codes int8 [B,N], scales float32 [B]) of x [B,N] (token-major) or [N,B] (feature-major), fp32 or bf16 on the GPU.
+
+    A weight matrix [M,N] is quantised row by row the same way.  New codes have a pitch of tsvd_int8_row_bytes(N).
+    """
+    return (_binding or _load_binding()).int8_quantize(x, x_layout, codes, scales, stream)
+
+
+def tsvd_int8_pack(codes, scales, dev_buf=None, stream=None) -> Int8Handle:
+    """Packs weights, codes int8 [M,N] and scales float32 [M] on the GPU, on their device; waits for the stream.  dev_buf: optional torch uint8 CUDA tensor."""
+    import torch
+    if not codes.is_cuda or codes.dtype != torch.int8 or codes.dim() != 2 or (codes.shape[1] > 1 and codes.stride(1) != 1):
+        raise ValueError("codes must be an int8 GPU tensor [M,N] with unit inner stride")
+    M, N = codes.shape
+    _need(scales, torch.float32, (M,), "scales")
+    if scales.device != codes.device or (dev_buf is not None and (dev_buf.device != codes.device or not dev_buf.is_contiguous())):
+        raise ValueError("scales and dev_buf must live on the codes' device, dev_buf contiguous")
+    out = _vp()
+    buf_ptr, buf_bytes = None, 0
+    if dev_buf is not None:
+        buf_ptr, buf_bytes = dev_buf.data_ptr(), dev_buf.numel() * dev_buf.element_size()
+    with torch.cuda.device(codes.device):
+        _check(load_library().tsvd_int8_pack(codes.data_ptr(), codes.stride(0) if M > 1 else N, scales.data_ptr(), M, N, buf_ptr, buf_bytes,
+                                             _stream(codes, stream), ctypes.byref(out)), "tsvd_int8_pack")
+    return Int8Handle(out.value, M, N, keepalive=dev_buf)
+
+
+def tsvd_int8_info(h: Int8Handle) -> dict:
+    vals = [_i64() for _ in range(2)]
+    _check(load_library().tsvd_int8_info(h.ptr, *[ctypes.byref(v) for v in vals]), "tsvd_int8_info")
+    return dict(zip(("M", "N"), (v.value for v in vals)))
+
+
+def tsvd_int8_workspace_bytes(h: Int8Handle, B: int, x_dtype: int, x_layout: int) -> int:
+    return int(load_library().tsvd_int8_workspace_bytes(h.ptr, B, x_dtype, x_layout))
+
+
+def tsvd_int8_forward(h: Int8Handle, x, x_layout=TSVD_FEATURE_MAJOR, bias=None, y=None, y_dtype=TSVD_F32, y_layout=TSVD_FEATURE_MAJOR,
+                      workspace=None, stream=None):
+    """y = W x + bias with the weights' 8-bit codes and x in 8 bits with a scale for each token; layouts, types, bias as tsvd_forward_io.
+
+    Without a workspace one is taken from torch's allocator; with a stream of the caller's own, y and workspace are the caller's own too.
+    """
+    return (_binding or _load_binding()).int8_layer(h, x, x_layout, bias, y, y_dtype, y_layout, workspace, stream)
+
+
+def tsvd_int8_product(h: Int8Handle, codes, scales, bias=None, y=None, y_dtype=TSVD_F32, y_layout=TSVD_FEATURE_MAJOR, stream=None):
+    """The same from codes int8 [B,N] (rows 16-byte aligned, as tsvd_int8_quantize makes them) and scales float32 [B]."""
+    return (_binding or _load_binding()).int8_product(h, codes, scales, bias, y, y_dtype, y_layout, stream)
+
+
+def tsvd_int8_free(h: Int8Handle) -> None:
+    if h is not None and getattr(h, "ptr", None):
+        load_library().tsvd_int8_free(h.ptr)
+        h.ptr = None
+
+
+# ---- group norm (include/tsvd_norm.h)
+def tsvd_group_norm_workspace_bytes(images: int, positions: int, C: int, groups: int) -> int:
+    return int(load_library().tsvd_group_norm_workspace_bytes(images, positions, C, groups))
+
+
+def tsvd_group_norm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, act: int = TSVD_ACT_NONE, y=None, y_dtype=None,
+                    y_layout=TSVD_TOKEN_MAJOR, workspace=None, stream=None):
+    """act(group norm) of x [images,positions,C] or [images,H,W,C] (channels last; [rows,C]: each row by itself), fp32 or bf16 on the GPU.
+
+    y has x's shape, or with y_layout=TSVD_FEATURE_MAJOR the channels first ([C,images,H,W], what tsvd_conv2d_forward reads); y_dtype: x's by default.
+    """
+    return (_binding or _load_binding()).group_norm(x, groups, gamma, beta, eps, act, y, _dtype_code(x) if y_dtype is None else y_dtype, y_layout,
+                                                    workspace, stream)
+
+
+def tsvd_group_norm_int8(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, act: int = TSVD_ACT_NONE, codes=None, scales=None,
+                         workspace=None, stream=None):
+    """The same as (codes int8 [images * positions,C], scales float32) for tsvd_int8_product."""
+    return (_binding or _load_binding()).group_norm_int8(x, groups, gamma, beta, eps, act, codes, scales, workspace, stream)
 
 
 def tsvd_free(h: Handle) -> None:

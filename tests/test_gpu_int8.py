@@ -1,0 +1,298 @@
+"""Layers in 8-bit integers against a plain implementation in 64 bits: codes and scales exactly, outputs to the three fp32 roundings that the
+formula leaves (the sum as a number, times the row's scale, times the token's scale plus bias), bf16 outputs to half a step more."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+SMALLEST = 2.0 ** -100
+
+
+@pytest.fixture(scope="module")
+def tsvd():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: the HIP path has no fallback")
+    import paper_2308_07641_amd as t
+    t.load_library()
+    return t
+
+
+def plain_codes(x):
+    """Codes, scales of x [B, N] (float64 array of fp32 / bf16 values)."""
+    a = np.maximum(np.abs(x).max(axis=1), SMALLEST)
+    scale, factor = (a / 127).astype(np.float32), (127 / a).astype(np.float32)
+    return np.rint(x * factor.astype(np.float64)[:, None]), scale
+
+
+def plain_layer(q, s, w, t, bias):
+    """(y, the part without bias) in 64 bits from codes and fp32 scales."""
+    p = (q @ w.T) * s.astype(np.float64)[:, None] * t.astype(np.float64)[None, :]
+    return p + (0 if bias is None else bias.astype(np.float64)[None, :]), p
+
+
+def allowed(y, p, bf16):
+    # (sum as a number, times t: half a step each; the last rounding half a step of y; second order: 2^-40)
+    tol = (2 * 2.0 ** -24 + 2.0 ** -40) * np.abs(p) + 2.0 ** -24 * np.abs(y) + 1e-44
+    return tol + (2.0 ** -8 * (np.abs(y) + tol) if bf16 else 0)
+
+
+def gpu_x(x, dtype, token_major, pitch=0, offset=0):
+    """x [B, N] on the GPU in either layout, with `pitch` more elements a row and an offset, both filled with NaN."""
+    import torch
+    v = torch.from_numpy(np.ascontiguousarray(x if token_major else x.T)).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    buf = torch.full((v.shape[0] * (v.shape[1] + pitch) + offset,), float("nan"), dtype=v.dtype, device="cuda:0")
+    view = buf[offset:].view(v.shape[0], v.shape[1] + pitch)[:, :v.shape[1]]
+    view.copy_(v)
+    return view, v.double().numpy() if token_major else v.double().numpy().T
+
+
+def values(rng, B, N, spread=True):
+    x = rng.standard_normal((B, N))
+    if spread:
+        x *= np.exp2(rng.integers(-20, 20, size=(B, 1)))
+        x[:, rng.integers(0, N, size=max(1, N // 50))] *= 30
+    return x
+
+
+SHAPES = [(1, 1), (1, 15), (3, 16), (2, 17), (5, 511), (4, 513), (3, 1025), (33, 100), (2, 2049), (3, 4097), (1, 8193), (2, 16385), (2, 131071), (70, 260)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("token_major", [True, False])
+@pytest.mark.parametrize("B,N", SHAPES)
+def test_codes_are_exact(tsvd, B, N, dtype, token_major):
+    import torch
+    print(f"case codes {B} {N} {dtype} {token_major}", flush=True)
+    rng = np.random.default_rng(B * 1000 + N)
+    for pitch, offset in ((0, 0), (3, 1)):
+        x, ref = gpu_x(values(rng, B, N), dtype, token_major, pitch, offset)
+        q, s = tsvd.tsvd_int8_quantize(x, x_layout=tsvd.TSVD_TOKEN_MAJOR if token_major else tsvd.TSVD_FEATURE_MAJOR)
+        torch.cuda.synchronize()
+        codes, scales = plain_codes(ref)
+        assert q.stride(0) == tsvd.tsvd_int8_row_bytes(N) or B == 1
+        assert np.array_equal(q.cpu().numpy().astype(np.float64), codes)
+        assert np.array_equal(s.cpu().numpy(), scales)
+
+
+def test_ties_go_to_the_even_code(tsvd):
+    import torch
+    x = torch.tensor([[127.0, 0.5, 1.5, 2.5, -0.5, -1.5, -126.5, 126.5, 0.49999997, -0.50000006]], device="cuda:0")
+    q, s = tsvd.tsvd_int8_quantize(x)
+    assert q.tolist() == [[127, 0, 2, 2, 0, -2, -126, 126, 0, -1]] and s.tolist() == [1.0]
+
+
+@pytest.mark.parametrize("token_major", [True, False])
+def test_zeros_tiny_values_and_values_that_are_no_numbers(tsvd, token_major):
+    import torch
+    N, M = 70, 20
+    x = torch.zeros((6, N))
+    x[1] = 2.0 ** -140
+    x[2, 3] = float("inf")
+    x[3, 69] = float("nan")
+    x[4] = torch.linspace(-3, 3, N)
+    x[5] = 3.0e38
+    g = x.to("cuda:0") if token_major else x.t().contiguous().to("cuda:0")
+    layout = tsvd.TSVD_TOKEN_MAJOR if token_major else tsvd.TSVD_FEATURE_MAJOR
+    q, s = tsvd.tsvd_int8_quantize(g, x_layout=layout)
+    assert not q[0].any() and not q[1].any() and torch.equal(q[5], torch.full((N,), 127, dtype=torch.int8, device="cuda:0"))
+    assert torch.isnan(s).tolist() == [False, False, True, True, False, False]
+    assert s[0].item() == s[1].item() == np.float32(SMALLEST / 127)
+    w = torch.randint(-127, 128, (M, N), dtype=torch.int8, device="cuda:0")
+    h = tsvd.tsvd_int8_pack(w, torch.full((M,), 2.0 ** -7, device="cuda:0"))
+    y = tsvd.tsvd_int8_forward(h, g, x_layout=layout, y_layout=tsvd.TSVD_TOKEN_MAJOR)
+    assert torch.isnan(y).all(1).tolist() == [False, False, True, True, False, False]
+    assert not torch.isnan(y[[0, 1, 4, 5]]).any() and not y[:2].any()
+    tsvd.tsvd_int8_free(h)
+
+
+# rows, features, tokens
+LAYERS = [(1, 1, 1), (16, 64, 1), (17, 65, 3), (100, 100, 16), (256, 256, 1), (300, 1000, 17), (1000, 2047, 33), (130, 4097, 64), (513, 520, 65), (48, 16385, 5), (33, 131071, 2),
+          (2000, 128, 300), (129, 127, 1025), (4100, 320, 1), (260, 4096, 31), (70, 9216, 130), (5000, 70, 2)]
+
+
+def layer(rng, M, N):
+    w = rng.integers(-127, 128, size=(M, N)).astype(np.int8)
+    w[0, 0] = -128                                  # (any code is allowed)
+    return w, (rng.random(M) * 1e-2 + 1e-4).astype(np.float32), rng.standard_normal(M).astype(np.float32)
+
+
+def packed(tsvd, w, t):
+    import torch
+    return tsvd.tsvd_int8_pack(torch.from_numpy(w).to("cuda:0"), torch.from_numpy(t).to("cuda:0"))
+
+
+@pytest.mark.parametrize("M,N,B", LAYERS)
+def test_layer_against_64_bits(tsvd, M, N, B):
+    import torch
+    rng = np.random.default_rng(M + 7 * N + 13 * B)
+    w, t, bias = layer(rng, M, N)
+    h = packed(tsvd, w, t)
+    x0 = values(rng, B, N)
+    b = torch.from_numpy(bias).to("cuda:0")
+    for dtype, x_tm, y_tm, y_bf16, with_bias, pitch in (("bf16", True, True, True, True, 0), ("f32", True, False, False, False, 5), ("bf16", False, False, True, True, 1),
+                                                        ("f32", False, True, False, True, 0), ("bf16", False, True, True, False, 8), ("bf16", True, False, False, True, 3)):
+        print(f"case layer {M} {N} {B} {dtype} x_tm={x_tm} y_tm={y_tm} bf16={y_bf16} bias={with_bias} pitch={pitch}", flush=True)
+        x, ref = gpu_x(x0, dtype, x_tm, pitch, pitch % 4)
+        codes, scales = plain_codes(ref)
+        want, p = plain_layer(codes, scales, w.astype(np.float64), t, bias if with_bias else None)
+        rows, cols = (B, M) if y_tm else (M, B)
+        full = torch.full((rows + 1, cols + pitch), 7.0, dtype=torch.bfloat16 if y_bf16 else torch.float32, device="cuda:0")
+        y = full[:rows, :cols]
+        y.fill_(float("nan"))
+        got = tsvd.tsvd_int8_forward(h, x, x_layout=tsvd.TSVD_TOKEN_MAJOR if x_tm else tsvd.TSVD_FEATURE_MAJOR, bias=b if with_bias else None, y=y,
+                                     y_dtype=tsvd.TSVD_BF16 if y_bf16 else tsvd.TSVD_F32, y_layout=tsvd.TSVD_TOKEN_MAJOR if y_tm else tsvd.TSVD_FEATURE_MAJOR)
+        torch.cuda.synchronize()
+        v = got.double().cpu().numpy()
+        v = v if y_tm else v.T
+        assert np.all(np.abs(v - want) <= allowed(want, p, y_bf16))
+        assert bool((full[rows:] == 7).all()) and bool((full[:, cols:] == 7).all())          # nothing written beside y
+        # the product from codes that are there: the same bits
+        q, s = tsvd.tsvd_int8_quantize(x, x_layout=tsvd.TSVD_TOKEN_MAJOR if x_tm else tsvd.TSVD_FEATURE_MAJOR)
+        again = tsvd.tsvd_int8_product(h, q, s, bias=b if with_bias else None, y_dtype=tsvd.TSVD_BF16 if y_bf16 else tsvd.TSVD_F32,
+                                       y_layout=tsvd.TSVD_TOKEN_MAJOR if y_tm else tsvd.TSVD_FEATURE_MAJOR)
+        assert torch.equal(again, got)
+    tsvd.tsvd_int8_free(h)
+
+
+def test_largest_sums_are_exact(tsvd):
+    """All codes at their ends: the sum reaches 2^31 - 2^14 and stays a whole number."""
+    import torch
+    N = 131071
+    w = torch.full((3, N), -128, dtype=torch.int8, device="cuda:0")
+    w[1] = 127
+    h = tsvd.tsvd_int8_pack(w, torch.ones(3, device="cuda:0"))
+    q = torch.full((2, tsvd.tsvd_int8_row_bytes(N)), -128, dtype=torch.int8, device="cuda:0")[:, :N]
+    y = tsvd.tsvd_int8_product(h, q, torch.ones(2, device="cuda:0"), y_layout=tsvd.TSVD_TOKEN_MAJOR)
+    want = torch.tensor([128 * 128 * N, -128 * 127 * N, 128 * 128 * N], dtype=torch.float64).float()
+    assert torch.equal(y.cpu(), want.expand(2, 3))
+    tsvd.tsvd_int8_free(h)
+
+
+@pytest.mark.parametrize("M,N", [(300, 520), (4096, 1024)])
+def test_a_token_does_not_depend_on_those_beside_it(tsvd, M, N):
+    import torch
+    rng = np.random.default_rng(5)
+    w, t, _ = layer(rng, M, N)
+    h = packed(tsvd, w, t)
+    x, _ = gpu_x(values(rng, 300, N), "bf16", True)
+    whole = tsvd.tsvd_int8_forward(h, x, x_layout=tsvd.TSVD_TOKEN_MAJOR, y_layout=tsvd.TSVD_TOKEN_MAJOR)
+    for b0, n in ((0, 1), (5, 2), (7, 16), (3, 17), (100, 40), (10, 64), (20, 65), (150, 129)):
+        part = tsvd.tsvd_int8_forward(h, x[b0:b0 + n], x_layout=tsvd.TSVD_TOKEN_MAJOR, y_layout=tsvd.TSVD_TOKEN_MAJOR)
+        assert torch.equal(part, whole[b0:b0 + n])
+    tsvd.tsvd_int8_free(h)
+
+
+def test_packing_into_the_callers_memory_and_from_rows_with_a_pitch(tsvd):
+    import torch
+    rng = np.random.default_rng(8)
+    M, N = 37, 75
+    w, t, _ = layer(rng, M, N)
+    wide = torch.full((M, N + 6), 99, dtype=torch.int8, device="cuda:0")
+    wide[:, 1:N + 1] = torch.from_numpy(w).to("cuda:0")
+    n = tsvd.tsvd_int8_packed_bytes(M, N)
+    buf = torch.full((n + 256,), 0xAB, dtype=torch.uint8, device="cuda:0")
+    h = tsvd.tsvd_int8_pack(wide[:, 1:N + 1], torch.from_numpy(t).to("cuda:0"), dev_buf=buf[:n])
+    assert tsvd.tsvd_int8_info(h) == {"M": M, "N": N}
+    assert bool((buf[n:] == 0xAB).all())
+    x, ref = gpu_x(values(rng, 4, N), "f32", True)
+    want, p = plain_layer(*plain_codes(ref), w.astype(np.float64), t, None)
+    y = tsvd.tsvd_int8_forward(h, x, x_layout=tsvd.TSVD_TOKEN_MAJOR, y_layout=tsvd.TSVD_TOKEN_MAJOR)
+    assert np.all(np.abs(y.double().cpu().numpy() - want) <= allowed(want, p, False))
+    tsvd.tsvd_int8_free(h)
+
+
+def test_weights_quantised_by_the_library(tsvd):
+    """W in fp32 -> codes and scales of its rows -> handle; y is within the two quantisations of W x: half a step of either, times the other."""
+    import torch
+    rng = np.random.default_rng(9)
+    M, N, B = 90, 333, 12
+    W = rng.standard_normal((M, N)).astype(np.float32)
+    q, s = tsvd.tsvd_int8_quantize(torch.from_numpy(W).to("cuda:0"))
+    h = tsvd.tsvd_int8_pack(q, s)
+    x, ref = gpu_x(values(rng, B, N, spread=False), "f32", True)
+    y = tsvd.tsvd_int8_forward(h, x, x_layout=tsvd.TSVD_TOKEN_MAJOR, y_layout=tsvd.TSVD_TOKEN_MAJOR).double().cpu().numpy()
+    sx, sw = np.abs(ref).max(1) / 127, np.abs(W).max(1) / 127
+    tol = 0.5 * sx[:, None] * np.abs(W).sum(1)[None, :] + 0.5 * sw[None, :] * np.abs(ref).sum(1)[:, None] + 0.25 * N * sx[:, None] * sw[None, :]
+    assert np.all(np.abs(y - ref @ W.T.astype(np.float64)) <= 1.001 * tol)
+    tsvd.tsvd_int8_free(h)
+
+
+@pytest.mark.parametrize("B,x_tm", [(1, False), (5, True), (40, False), (200, True)])
+def test_captured_and_replayed(tsvd, B, x_tm):
+    import torch
+    rng = np.random.default_rng(11)
+    M, N = 520, 770
+    w, t, bias = layer(rng, M, N)
+    h = packed(tsvd, w, t)
+    b = torch.from_numpy(bias).to("cuda:0")
+    x, _ = gpu_x(values(rng, B, N), "bf16", x_tm)
+    xl = tsvd.TSVD_TOKEN_MAJOR if x_tm else tsvd.TSVD_FEATURE_MAJOR
+    ws = [torch.empty(max(256, tsvd.tsvd_int8_workspace_bytes(h, B, tsvd.TSVD_BF16, xl)), dtype=torch.uint8, device="cuda:0") for _ in range(2)]
+    ys = [torch.empty((M, B), device="cuda:0") for _ in range(2)]
+    graphs = []
+    for k in range(2):                               # two graphs of one handle, workspaces of their own
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            tsvd.tsvd_int8_forward(h, x, x_layout=xl, bias=b, y=ys[k], workspace=ws[k])
+        graphs.append(g)
+    for r in range(3):
+        new, _ = gpu_x(values(rng, B, N), "bf16", x_tm)
+        x.copy_(new)
+        for k in range(2):
+            ys[k].fill_(float("nan"))
+            ws[k].fill_(0xFF)
+            graphs[k].replay()
+        torch.cuda.synchronize()
+        want = tsvd.tsvd_int8_forward(h, x, x_layout=xl, bias=b)
+        assert torch.equal(ys[0], want) and torch.equal(ys[1], want)
+    tsvd.tsvd_int8_free(h)
+
+
+def test_calls_of_one_handle_on_two_streams(tsvd):
+    import torch
+    rng = np.random.default_rng(12)
+    M, N = 1000, 1500
+    w, t, _ = layer(rng, M, N)
+    h = packed(tsvd, w, t)
+    xs = [gpu_x(values(rng, B, N), "bf16", True)[0] for B in (3, 200)]
+    want = [tsvd.tsvd_int8_forward(h, x, x_layout=1) for x in xs]
+    ys = [torch.empty_like(v) for v in want]
+    ws = [torch.empty(max(256, tsvd.tsvd_int8_workspace_bytes(h, x.shape[0], tsvd.TSVD_BF16, 1)), dtype=torch.uint8, device="cuda:0") for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for k in range(2):
+            tsvd.tsvd_int8_forward(h, xs[k], x_layout=1, y=ys[k], workspace=ws[k], stream=streams[k].cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ys, want))
+    tsvd.tsvd_int8_free(h)
+
+
+def test_refusals(tsvd):
+    import torch
+    h = tsvd.tsvd_int8_pack(torch.zeros((8, 32), dtype=torch.int8, device="cuda:0"), torch.ones(8, device="cuda:0"))
+    x = torch.zeros((4, 32), device="cuda:0")
+    ok = dict(x_layout=tsvd.TSVD_TOKEN_MAJOR)
+    for bad in (dict(x=x[:, :31]), dict(x=x.half()), dict(x=x.t()), dict(x=x.cpu()), dict(bias=torch.zeros(7, device="cuda:0")), dict(bias=torch.zeros(8)),
+                dict(y=torch.zeros((8, 5), device="cuda:0")), dict(y=torch.zeros((8, 4), dtype=torch.bfloat16, device="cuda:0")),
+                dict(workspace=torch.zeros(64, dtype=torch.uint8)), dict(stream=torch.cuda.Stream().cuda_stream), dict(x=x[:0])):
+        args = dict(ok, x=x)
+        args.update(bad)
+        with pytest.raises((ValueError, TypeError, tsvd.TsvdError)):
+            tsvd.tsvd_int8_forward(h, **args)
+    q, s = tsvd.tsvd_int8_quantize(x)
+    y = torch.full((8, 4), 5.0, device="cuda:0")
+    flat = torch.zeros((4, 33), dtype=torch.int8, device="cuda:0")
+    for codes, scales in ((flat[:, :32], s), (flat.view(-1)[1:129].view(4, 32), s), (q[:, :16], s), (q.float(), s), (q, s[:3]), (q, s.double())):
+        with pytest.raises((ValueError, TypeError, tsvd.TsvdError)):
+            tsvd.tsvd_int8_product(h, codes, scales, y=y)
+    # a single row of codes whose last piece would pass the end of its memory
+    h2 = tsvd.tsvd_int8_pack(torch.zeros((8, 30), dtype=torch.int8, device="cuda:0"), torch.ones(8, device="cuda:0"))
+    with pytest.raises(ValueError):
+        tsvd.tsvd_int8_product(h2, torch.zeros((1, 30), dtype=torch.int8, device="cuda:0"), s[:1])
+    assert bool((y == 5).all())
+    tsvd.tsvd_int8_free(h)
+    with pytest.raises(tsvd.TsvdError):
+        tsvd.tsvd_int8_forward(h, x, x_layout=tsvd.TSVD_TOKEN_MAJOR)
+    tsvd.tsvd_int8_free(h2)

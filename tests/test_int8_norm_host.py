@@ -1,0 +1,93 @@
+"""CPU-only tests of the layers in 8-bit integers and of the group norm: exported symbols, sizes, and refusals, which all come before any device work."""
+import ctypes
+import os
+import re
+
+import pytest
+
+import paper_2308_07641_amd as tsvd
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_every_declared_function_is_exported_and_bound():
+    lib = tsvd.load_library()
+    for header in ("tsvd_int8.h", "tsvd_norm.h"):
+        text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", header)).read(), flags=re.S)
+        names = set(re.findall(r"\b(tsvd_[a-z0-9_]+)\s*\(", text))
+        assert names
+        for n in names:
+            assert hasattr(lib, n) and hasattr(tsvd, n), n
+
+
+def test_sizes():
+    assert [tsvd.tsvd_int8_row_bytes(n) for n in (0, -1, 1, 128, 129, 131071, 131072)] == [0, 0, 128, 128, 256, 131072, 0]
+    assert tsvd.tsvd_int8_packed_bytes(1, 1) == 256 + 2048 and tsvd.tsvd_int8_packed_bytes(17, 129) == 256 + 2 * 4 * 1024
+    assert tsvd.tsvd_int8_packed_bytes(0, 5) == 0 and tsvd.tsvd_int8_packed_bytes(5, 0) == 0 and tsvd.tsvd_int8_packed_bytes(5, 1 << 17) == 0
+    assert tsvd.tsvd_int8_packed_bytes((1 << 24) + 1, 4) == 0
+    for bad in ((0, 1, 1, 1), (1, 0, 1, 1), (1, 1, 0, 1), (1, 1, 1, 0), (1, 1, 6, 4), (1, 1, (1 << 20) + 1, 1), (1 << 16, 1 << 15, 8, 1)):
+        assert tsvd.tsvd_group_norm_workspace_bytes(*bad) == 0
+    assert tsvd.tsvd_group_norm_workspace_bytes(1, 1, 8, 1) >= 256
+
+
+EINVAL, EUNSUPPORTED = 1, 5
+
+
+def test_int8_calls_check_their_arguments_first():
+    lib = tsvd.load_library()
+    buf = (ctypes.c_char * 4096)()
+    p = (ctypes.addressof(buf) + 255) // 256 * 256
+    out = ctypes.c_void_p()
+
+    def quantize(x=p, dtype=0, layout=1, B=2, N=32, ldx=32, codes=p, ldq=32, s=p):
+        return lib.tsvd_int8_quantize(x, dtype, layout, B, N, ldx, codes, ldq, s, None)
+
+    for bad in (dict(x=None), dict(codes=None), dict(s=None), dict(dtype=2), dict(layout=2), dict(B=0), dict(N=0), dict(ldx=31), dict(layout=0, ldx=1), dict(ldq=31), dict(ldq=40),
+                dict(codes=p + 8)):
+        assert quantize(**bad) == EINVAL, bad
+    assert quantize(N=1 << 17, ldx=1 << 17, ldq=1 << 17) == EUNSUPPORTED and quantize(B=(1 << 24) + 1) == EUNSUPPORTED
+
+    def pack(w=p, ldw=32, t=p, M=4, N=32, d=None, nbytes=0, o=ctypes.byref(out)):
+        return lib.tsvd_int8_pack(w, ldw, t, M, N, d, nbytes, None, o)
+
+    for bad in (dict(w=None), dict(t=None), dict(o=None), dict(M=0), dict(N=0), dict(ldw=31), dict(d=p, nbytes=100), dict(d=p + 64, nbytes=1 << 20), dict(nbytes=5)):
+        assert pack(**bad) == EINVAL, bad
+    assert pack(N=1 << 17, ldw=1 << 17) == EUNSUPPORTED and pack(M=(1 << 24) + 1) == EUNSUPPORTED
+    assert out.value is None
+    assert lib.tsvd_int8_info(None, None, None) == EINVAL
+    assert lib.tsvd_int8_workspace_bytes(None, 4, 0, 0) == 0
+    assert lib.tsvd_int8_product(None, p, 32, p, 1, None, p, 0, 0, 1, None) == EINVAL
+    assert lib.tsvd_int8_forward(None, p, 0, 0, 1, 1, None, p, 0, 0, 1, p, 4096, None) == EINVAL
+    lib.tsvd_int8_free(None)
+
+
+def test_norm_calls_check_their_arguments_first():
+    lib = tsvd.load_library()
+    buf = (ctypes.c_char * 8192)()
+    p = (ctypes.addressof(buf) + 255) // 256 * 256
+    nan, inf = float("nan"), float("inf")
+
+    def norm(x=p, dtype=0, images=1, P=2, C=32, ldx=32, groups=4, eps=1e-5, act=0, y=p, y_dtype=0, y_layout=1, ldy=32, ws=p, nbytes=4096):
+        return lib.tsvd_group_norm(x, dtype, images, P, C, ldx, groups, None, None, eps, act, y, y_dtype, y_layout, ldy, ws, nbytes, None)
+
+    shared = (dict(x=None), dict(y=None), dict(dtype=2), dict(images=0), dict(P=0), dict(C=0), dict(groups=0), dict(groups=5), dict(ldx=31), dict(eps=0.0), dict(eps=-1.0), dict(eps=nan),
+              dict(eps=inf), dict(act=-1), dict(act=4), dict(ws=None), dict(ws=p + 8), dict(nbytes=0))
+    for bad in shared + (dict(y_dtype=2), dict(y_layout=2), dict(ldy=31), dict(y_layout=0, ldy=1)):
+        assert norm(**bad) == EINVAL, bad
+    assert norm(C=1 << 21, ldx=1 << 21, ldy=1 << 21) == EUNSUPPORTED and norm(images=1 << 20, P=1 << 12) == EUNSUPPORTED
+
+    def codes(x=p, dtype=0, images=1, P=2, C=32, ldx=32, groups=4, eps=1e-5, act=0, y=p, ldq=32, s=p, ws=p, nbytes=4096):
+        return lib.tsvd_group_norm_int8(x, dtype, images, P, C, ldx, groups, None, None, eps, act, y, ldq, s, ws, nbytes, None)
+
+    for bad in shared + (dict(s=None), dict(y=p + 8), dict(ldq=31), dict(ldq=16), dict(ldq=40)):
+        assert codes(**bad) == EINVAL, bad
+
+
+def test_packing_needs_a_device():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present")
+    out = ctypes.c_void_p()
+    buf = (ctypes.c_char * 4096)()
+    p = ctypes.addressof(buf)
+    assert tsvd.load_library().tsvd_int8_pack(p, 32, p, 4, 32, None, 0, None, ctypes.byref(out)) == 4 and out.value is None

@@ -12,6 +12,7 @@
 #define TSVD_INT8_MAX_N ((1 << 17) - 1)
 #define TSVD_INT8_MAX_M (1 << 24)
 #define TSVD_INT8_MAX_B (1 << 24)
+#define TSVD_INT8_MAX_PITCH (1 << 22)                // of codes that a product reads: 256 rows within 32-bit places
 #define TSVD_INT8_FLOOR 7.888609052210118e-31f       // 2^-100: the largest magnitude that a token is scaled by at least
 
 struct tsvd_int8_handle {

@@ -259,7 +259,7 @@ extern "C" tsvd_status tsvd_int8_product(const tsvd_int8_handle* h, const int8_t
                                          const float* bias_dev, void* y_dev, tsvd_dtype y_dtype, tsvd_layout y_layout, int64_t ldy, void* stream) {
     if (!h || !scales_dev || !y_dev || B < 1 || bad_dtype(y_dtype) || bad_layout(y_layout)) return TSVD_EINVAL;
     if (bad_codes(codes_dev, ldq, h->N) || ldy < (y_layout == TSVD_TOKEN_MAJOR ? h->M : B)) return TSVD_EINVAL;
-    if (B > TSVD_INT8_MAX_B) return TSVD_EUNSUPPORTED;
+    if (B > TSVD_INT8_MAX_B || ldq > TSVD_INT8_MAX_PITCH) return TSVD_EUNSUPPORTED;
     const tsvd_int8_problem p = {h, codes_dev, ldq, scales_dev, B, bias_dev, y_dev, y_dtype == TSVD_BF16, y_layout == TSVD_TOKEN_MAJOR, ldy};
     return tsvd_int8_gemm(p, static_cast<hipStream_t>(stream)) == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
 }

@@ -261,7 +261,8 @@ extern "C" tsvd_status tsvd_int8_product(const tsvd_int8_handle* h, const int8_t
     if (bad_codes(codes_dev, ldq, h->N) || ldy < (y_layout == TSVD_TOKEN_MAJOR ? h->M : B)) return TSVD_EINVAL;
     if (B > TSVD_INT8_MAX_B || ldq > TSVD_INT8_MAX_PITCH) return TSVD_EUNSUPPORTED;
     const tsvd_int8_problem p = {h, codes_dev, ldq, scales_dev, B, bias_dev, y_dev, y_dtype == TSVD_BF16, y_layout == TSVD_TOKEN_MAJOR, ldy};
-    return tsvd_int8_gemm(p, static_cast<hipStream_t>(stream)) == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
+    const hipError_t e = tsvd_int8_stream_serves(*h, B) ? tsvd_int8_stream(p, static_cast<hipStream_t>(stream)) : tsvd_int8_gemm(p, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
 }
 
 extern "C" size_t tsvd_int8_workspace_bytes(const tsvd_int8_handle* h, int64_t B, tsvd_dtype x_dtype, tsvd_layout x_layout) {
@@ -276,6 +277,10 @@ extern "C" tsvd_status tsvd_int8_forward(const tsvd_int8_handle* h, const void* 
     if (ldx < (x_layout == TSVD_TOKEN_MAJOR ? h->N : B) || ldy < (y_layout == TSVD_TOKEN_MAJOR ? h->M : B)) return TSVD_EINVAL;
     if (B > TSVD_INT8_MAX_B) return TSVD_EUNSUPPORTED;
     if (!workspace || workspace_bytes < tsvd_int8_workspace_bytes(h, B, x_dtype, x_layout) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return TSVD_EINVAL;
+    if (one_row(x_layout, B, ldx) && tsvd_int8_stream_makes(*h, B)) {
+        const tsvd_int8_problem p = {h, nullptr, 0, nullptr, B, bias_dev, y_dev, y_dtype == TSVD_BF16, y_layout == TSVD_TOKEN_MAJOR, ldy};
+        return tsvd_int8_stream_from(p, x_dev, x_dtype == TSVD_BF16, ldx, static_cast<hipStream_t>(stream)) == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
+    }
     int8_t* codes = static_cast<int8_t*>(workspace);
     float* scales = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + codes_bytes(h, B));
     const int64_t ldq = (int64_t)tsvd_int8_row_bytes(h->N);

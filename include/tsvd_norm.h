@@ -40,7 +40,7 @@ size_t tsvd_group_norm_workspace_bytes(int64_t images, int64_t positions, int64_
  *   workspace : device, at least tsvd_group_norm_workspace_bytes(...) bytes, 256-byte aligned; contents undefined afterwards.
  * x, y and workspace must not alias.
  * TSVD_EINVAL: null pointers, sizes below 1, groups that do not divide C, strides that are too small, an unknown type, layout or activation.
- * TSVD_EUNSUPPORTED: C > 2^20, images * positions > 2^31 - 1. */
+ * TSVD_EUNSUPPORTED: C > 2^20, groups > 4096, images * positions > 2^31 - 1. */
 tsvd_status tsvd_group_norm(const void* x_dev, tsvd_dtype x_dtype, int64_t images, int64_t positions, int64_t C, int64_t ldx, int64_t groups,
                             const float* gamma_dev, const float* beta_dev, float eps, tsvd_activation act, void* y_dev, tsvd_dtype y_dtype,
                             tsvd_layout y_layout, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);

@@ -1,13 +1,18 @@
 // Group norm with an activation, channels last (include/tsvd_norm.h).
 //
-// Bound by memory: x once for the statistics, once more for y where an image does not stay on the chip, y once.  Statistics: a workgroup holds a
-// piece of one image and of whole groups in registers, takes the sum of each of its groups, then the squares of the deviations from the piece's own mean, so that
-// nothing cancels; pieces are joined by n (mean - common mean)^2.  Every sum has a fixed order.
+// Bound by memory: x once and y once where a workgroup can hold what it normalises, else x twice.  A thread keeps eight neighbouring channels and walks along the
+// positions: sums of x - k and (x - k)^2 for each channel, k being the first value that it meets.  As k is one of the values, the deviations that cancel are
+// part of the result: the sum of squares about the thread's own mean is right to the number of its values times 2^-24, whatever the values are.  Threads, and
+// pieces of an image, are then joined by n (mean - common mean)^2, never by a difference of squares.  Every sum has a fixed order.
+//
+// Forms: rows (one position and one group: a row in registers), one launch (a workgroup has all positions of an image for some groups), and two launches (statistics
+// of pieces; y, every workgroup joining the pieces that it needs).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "../../include/tsvd_norm.h"
 #include "tsvd_epilogue.h"
@@ -17,7 +22,9 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Rows of one thread at most in the statistics, and with the eight channels of a vector the values behind one k: what their error grows with.
+constexpr int MAX_ROWS = 64;
 
 struct norm_args {
     const void* x;
@@ -29,288 +36,755 @@ struct norm_args {
     int act;
     void* y;
     long long ldy;
-    int out_bf16;
+    int out_bf16, token_major;
     float* scales;                // int8 output
     float4* parts;                // [images][G][chunks]: mean, sum of squared deviations, values
-    float2* stats;                // [images][G]: mean, 1 / sqrt(v + eps)
-    long long chunks;             // pieces of an image along its positions (one group a workgroup: along its vectors)
-    int gpb, nblk;                // groups of a workgroup, workgroups side by side along the channels
-    int rows;                     // positions of a piece, where a workgroup holds several groups
+    long long chunks;             // pieces of an image along its positions (single groups: along its vectors)
+    int gpb, nblk;                // statistics: groups of a workgroup, workgroups side by side along the channels
+    int rows;                     // positions of a piece
+    int vecs, vblk;               // y: vectors of a workgroup, workgroups side by side
+    long long y_rows, y_chunks;   // y: positions of a workgroup, workgroups one behind the other
 };
 
-__device__ __forceinline__ float norm_act(float h, int act) {
-    if (act == TSVD_ACT_RELU) return h > 0.f ? h : h != h ? h : 0.f;
-    if (act == TSVD_ACT_SILU) return h / (1.f + __expf(-h));
-    if (act == TSVD_ACT_GELU) return 0.5f * h * (1.f + erff(h * 0.70710678118654752f));
-    return h;
+// a / b for 0 <= a < 2^20, b >= 1: (a + 1/2) / b is 1 / (2 b) away from a whole number at least, more than the two roundings.  (A division of integers takes some forty
+// instructions, one of 64 bits hundreds, and everything here waits for them.)
+__device__ __forceinline__ int quotient(int a, int b) { return (int)(((float)a + 0.5f) * __builtin_amdgcn_rcpf((float)b)); }
+
+// erfc(a) for a >= 0 to 1.5e-7 (Abramowitz and Stegun, 7.1.26).
+__device__ __forceinline__ float norm_erfc(float a) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.f));
+    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    return poly * __expf(-a * a);
+}
+// act of eight values (act is the same for the whole launch: one branch for all of them)
+__device__ __forceinline__ void norm_act(float (&f)[8], int act) {
+    if (act == TSVD_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= __builtin_amdgcn_rcpf(1.f + __expf(-f[e]));
+    } else if (act == TSVD_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float c = norm_erfc(fabsf(f[e]) * 0.70710678118654752f);
+            f[e] *= f[e] > 0.f ? fmaf(-0.5f, c, 1.f) : 0.5f * c;
+        }
+    } else if (act == TSVD_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = f[e] < 0.f ? 0.f : f[e];          // (NaN stays)
+    }
 }
 
-// ---- statistics ------------------------------------------------------------------------------------
-// T threads, NV vectors of eight channels each.  Several groups in a workgroup: a thread keeps one vector of the block's channels and takes every T / (vectors)-th position;
-// ONE group: vectors of the piece in order, whatever position they belong to.
-template <typename X, int T, int NV, bool ONE>
-__global__ void __launch_bounds__(T)
-norm_stats_kernel(norm_args p) {
-    __shared__ float part[ONE ? 64 : T * 9];
-    __shared__ float channel[ONE ? 1 : T * 8];
-    __shared__ float mean_of[ONE ? 1 : T * 8];
-    const int tid = threadIdx.x;
-    const long long items = p.images * p.nblk * p.chunks;
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long chunk = item % p.chunks, rest = item / p.chunks, image = rest / p.nblk;
-        const int blk = (int)(rest % p.nblk);
-        const X* x = static_cast<const X*>(p.x) + image * p.P * p.ldx;
-        int8_eight<X> v[NV];
-        if constexpr (ONE) {
-            const int c0 = blk * p.cg, cvec = (p.cg + 7) / 8;
-            const long long first = chunk * (T * NV) + tid, total = p.P * cvec;
-            long long pos = first / cvec;
-            int at = (int)(first - pos * cvec);
-            const int step_p = T / cvec, step_v = T % cvec;
-            int n[NV];
+// What a thread multiplies and adds for its eight channels: gamma and beta first (they do not wait for the statistics), then the groups' mean and 1 / sqrt(v + eps).
+struct norm_channels {
+    float mean[8], factor[8], beta[8];
+    __device__ __forceinline__ void load(const norm_args& p, int c0, int n) {
+        int8_eight<float> g, b;
+        b.zero();
+        if (p.beta) b = int8_load8(p.beta + c0, 0, n);
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                n[k] = pos < p.P ? min(8, p.cg - 8 * at) : 0;
-                v[k].zero();
-                if (n[k]) v[k] = int8_load8(x + pos * p.ldx + c0, 8 * at, p.cg);
-                at += step_v, pos += step_p;
-                if (at >= cvec) at -= cvec, ++pos;
-            }
-            (void)total;
-            float sum = 0.f;
-            int count = 0;
+        for (int e = 0; e < 8; ++e) beta[e] = b.get(e), factor[e] = 1.f;
+        if (p.gamma) {
+            g = int8_load8(p.gamma + c0, 0, n);
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                count += n[k];
+            for (int e = 0; e < 8; ++e) factor[e] = g.get(e);
+        }
+    }
+    // n channels from c0 on; of groups from g0 on
+    __device__ __forceinline__ void set(int cg, int c0, int n, int g0, const float* mean_of, const float* rstd_of) {
+        const int first = quotient(c0, cg);
+        int g = first - g0, left = cg - (c0 - first * cg);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += v[k].get(e);          // (zeros behind the end)
-            }
-            auto reduce = [&](float a) {
-                for (int m = 32; m > 0; m >>= 1) a += __shfl_xor(a, m);
-                __syncthreads();
-                if ((tid & 63) == 0) part[tid >> 6] = a;
-                __syncthreads();
-                a = 0.f;
+        for (int e = 0; e < 8; ++e) {
+            const int at = e < n ? g : 0;
+            mean[e] = mean_of[at];
+            factor[e] *= rstd_of[at];
+            if (--left == 0) ++g, left = cg;
+        }
+    }
+    __device__ __forceinline__ void set(float m, float rstd) {
 #pragma unroll
-                for (int w = 0; w < T / 64; ++w) a += part[w];
-                return a;
-            };
-            const float cnt = reduce((float)count), mean = reduce(sum) / cnt;
-            float m2 = 0.f;
+        for (int e = 0; e < 8; ++e) mean[e] = m, factor[e] *= rstd;
+    }
+    template <typename X>
+    __device__ __forceinline__ void apply(const int8_eight<X>& v, int act, float (&f)[8]) const {
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
+        for (int e = 0; e < 8; ++e) f[e] = fmaf(v.get(e) - mean[e], factor[e], beta[e]);
+        norm_act(f, act);
+    }
+};
+
+// N rows of a vector, from `pos` on in steps: loads that all go out together.  WHOLE: all eight channels exist; no branch stands between the loads then, and
+// rows at or behind the end are the last one again (not used).
+template <bool WHOLE, int N, typename X>
+__device__ __forceinline__ void load_rows(int8_eight<X> (&u)[N], const X* x, long long ldx, int at, int valid, int pos, int step, int end) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float d = e < n[k] ? v[k].get(e) - mean : 0.f;
-                    m2 = fmaf(d, d, m2);
-                }
-            m2 = reduce(m2);
-            if (tid == 0) p.parts[(image * p.G + blk) * p.chunks + chunk] = float4{mean, m2, cnt, 0.f};
+    for (int k = 0; k < N; ++k) {
+        const X* row = x + (long long)min(pos + k * step, end - 1) * ldx;
+        if constexpr (WHOLE) u[k].load(row + at);
+        else u[k] = int8_load8(row, at, valid);
+    }
+}
+template <typename F>
+__device__ __forceinline__ void whole_or_not(int channels, F&& body) {
+    if (channels % 8 == 0) body(std::true_type());
+    else body(std::false_type());
+}
+
+// n values side by side (token-major y)
+__device__ __forceinline__ void store8(void* y, size_t at, const float (&f)[8], int n, int out_bf16) {
+    if (n >= 8) {
+        if (out_bf16) {
+            typedef u32x4 u32x4_at __attribute__((aligned(2)));
+            *reinterpret_cast<u32x4_at*>(static_cast<uint16_t*>(y) + at) = u32x4{tsvd_pack_bf16(f[0], f[1]), tsvd_pack_bf16(f[2], f[3]), tsvd_pack_bf16(f[4], f[5]), tsvd_pack_bf16(f[6], f[7])};
         } else {
-            const int g0 = blk * p.gpb, ng = min(p.gpb, p.G - g0), c0 = g0 * p.cg, nch = ng * p.cg, cvec = (nch + 7) / 8;
-            const int R = T / cvec, at = tid % cvec, r = tid / cvec;
-            const long long p0 = chunk * p.rows;
-            const int rows = (int)min((long long)p.rows, p.P - p0);
-            const bool active = r < R;
-            float sum[8] = {};
+            typedef f32x4 f32x4_at __attribute__((aligned(4)));
+            *reinterpret_cast<f32x4_at*>(static_cast<float*>(y) + at) = f32x4{f[0], f[1], f[2], f[3]};
+            *reinterpret_cast<f32x4_at*>(static_cast<float*>(y) + at + 4) = f32x4{f[4], f[5], f[6], f[7]};
+        }
+    } else {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                v[k].zero();
-                const int pos = r + k * R;
-                if (active && pos < rows) v[k] = int8_load8(x + (p0 + pos) * p.ldx + c0, 8 * at, nch);
+        for (int e = 0; e < 7; ++e)
+            if (e < n) tsvd_store_y(y, at + e, f[e], out_bf16);
+    }
+}
+// ... and in rows of their own (feature-major y)
+__device__ __forceinline__ void store8_apart(void* y, int c0, long long ldy, long long row, const float (&f)[8], int n, int out_bf16) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += v[k].get(e);
+    for (int e = 0; e < 8; ++e)
+        if (e < n) tsvd_store_y(y, (size_t)(c0 + e) * ldy + row, f[e], out_bf16);
+}
+
+__device__ __forceinline__ uint2 codes_of(const float (&f)[8], float factor) {
+    uint32_t c[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = int8_code(f[e], factor);
+    return uint2{int8_pack4(c[0], c[1], c[2], c[3]), int8_pack4(c[4], c[5], c[6], c[7])};
+}
+
+// ---- sums ------------------------------------------------------------------------------------------
+// Of one channel and thread: values about the first of them.
+struct norm_sums {
+    float k[8], s1[8], s2[8];
+    int n;
+    __device__ __forceinline__ void clear() {
+        n = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) k[e] = s1[e] = s2[e] = 0.f;
+    }
+    template <typename X>
+    __device__ __forceinline__ void add(const int8_eight<X>& v) {
+        if (n++ == 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) k[e] = v.get(e);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float d = v.get(e) - k[e];
+            s1[e] += d;
+            s2[e] = fmaf(d, d, s2[e]);
+        }
+    }
+};
+
+// What the threads of a workgroup know of its groups, in LDS: a thread (row r of R, vector `at` of cvec) leaves mean, sum of squares and number of its values of every
+// group g that its eight channels belong to.  Going along a row either the vector or the group is the next one, so at + g is a place of its own.
+struct norm_piece {
+    float mean, m2, n;
+};
+struct norm_lds {
+    norm_piece* piece;            // [R][cvec + ng]
+    float *mean, *m2;             // [ng]: of the groups
+    __device__ __forceinline__ norm_lds(float* base, int ng, int R, int cvec) : piece(reinterpret_cast<norm_piece*>(base + 2 * ng)), mean(base), m2(base + ng) {}
+    static size_t bytes(int ng, int R, int cvec) { return 8 * (size_t)ng + sizeof(norm_piece) * (size_t)R * (cvec + ng); }
+};
+// Lanes that join one of ng groups, T threads in all: a power of two up to 64.
+__device__ __forceinline__ int lanes_log2(int ng, int T) {
+    int log = 6;
+    while (log > 0 && (ng << log) > T) --log;
+    return log;
+}
+// Numbers, sums and sums of squares of 2^log lanes -> mean, and the sum of squared deviations or 1 / sqrt(v + eps).
+template <bool FINAL>
+__device__ __forceinline__ void store_joined(double n, double sum, double sq, int log, float eps, bool mine, float* mean, float* m2) {
+    for (int m = 1 << log >> 1; m > 0; m >>= 1) n += __shfl_xor(n, m), sum += __shfl_xor(sum, m), sq += __shfl_xor(sq, m);
+    if (!mine) return;
+    // (n is a whole number: its reciprocal in fp32, corrected once, is right to 2^-46)
+    const double r0 = __builtin_amdgcn_rcpf((float)n), inv = r0 * (2.0 - n * r0), mu = sum * inv, dev = sq - sum * mu;
+    *mean = (float)mu;
+    if constexpr (FINAL) {
+        const float v = (float)(dev * inv);
+        *m2 = __builtin_amdgcn_rsqf((v < 0.f ? 0.f : v) + eps);       // (a variance that is no number stays none)
+    } else {
+        *m2 = (float)dev;
+    }
+}
+// Means and sums of squared deviations of the workgroup's groups from its threads' sums.  The pieces are added up as sums of values and squares in 64 bits: what
+// cancels there is 2^-53 of the mean's square.
+// (FINAL: 1 / sqrt(v + eps) in the place of the sum of squares)
+template <int T, bool FINAL>
+__device__ __forceinline__ void join_threads(const norm_lds& l, const norm_sums& s, int at, int r, int cvec, int R, int nch, int ng, int cg, float eps) {
+    const int tid = threadIdx.x;
+    if (r < R) {
+        const float n = (float)s.n, inv = s.n ? __builtin_amdgcn_rcpf(n) : 0.f;
+        norm_piece* to = l.piece + r * (cvec + ng) + at;
+        int g = quotient(8 * at, cg), left = cg - (8 * at - g * cg);
+        float first = 0.f, sum = 0.f, m2 = 0.f, count = 0.f;
+        // a group's channels in this vector: their means about the first of them
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (8 * at + e < nch) {
+                const float mean = fmaf(s.s1[e], inv, s.k[e]);
+                if (count == 0.f) first = mean;
+                const float d = mean - first;
+                sum += d;
+                m2 += fmaf(n * d, d, fmaf(-s.s1[e] * inv, s.s1[e], s.s2[e]));
+                count += 1.f;
+                if (--left == 0 || e == 7 || 8 * at + e == nch - 1) {
+                    const float off = sum * __builtin_amdgcn_rcpf(count);
+                    to[g] = norm_piece{first + off, fmaf(-n * sum, off, m2), n * count};
+                    ++g, left = cg;
+                    sum = m2 = count = 0.f;
+                }
             }
-            // the sums of the threads of a channel, then of the channels of a group (L lanes for each)
-            int L = 64;
-            while (L * ng > T && L > 1) L >>= 1;
-            auto by_group = [&](const float (&a)[8], float* out) {
-                __syncthreads();
-                if (active)
+        }
+    }
+    __syncthreads();
+    const int log = lanes_log2(ng, T), L = 1 << log, lane = tid & (L - 1);
+    for (int g = tid >> log; g < ((ng + (T >> log) - 1) & -(T >> log)); g += T >> log) {       // (whole wavefronts)
+        double n = 0, sum = 0, sq = 0;
+        if (g < ng) {
+            const int a0 = (g * cg) >> 3, nv = ((g * cg + cg - 1) >> 3) - a0 + 1, step_r = quotient(L, nv), step_k = L - step_r * nv;
+            int row = quotient(lane, nv), k = lane - row * nv;
+            const norm_piece* from = l.piece + a0 + g;
+            while (row < R) {
+                const norm_piece q = from[row * (cvec + ng) + k];
+                n += q.n, sum += (double)q.n * q.mean, sq += q.m2 + (double)q.n * q.mean * q.mean;
+                row += step_r, k += step_k;
+                if (k >= nv) k -= nv, ++row;
+            }
+        }
+        store_joined<FINAL>(n, sum, sq, log, eps, g < ng && lane == 0, l.mean + g, l.m2 + g);
+    }
+    __syncthreads();
+}
+
+// ---- one launch: a workgroup has the groups blk gpb ... of an image, all positions ----------------------------
+// NV: rows of a thread at most, held in registers.
+template <typename X, int T, int NV>
+__global__ void __launch_bounds__(T)
+norm_one_kernel(norm_args p) {
+    extern __shared__ __align__(16) float smem[];
+    const int tid = threadIdx.x;
+    const uint32_t items = (uint32_t)(p.images * p.nblk), each = items >> 3, more = items & 7;
+    for (uint32_t id = blockIdx.x; id < items; id += gridDim.x) {
+        // workgroups go round the XCDs: each gets a run of the items, so that the groups of an image, which share lines of x and y, meet in one L2
+        const uint32_t item = (id & 7) * each + min(id & 7, more) + (id >> 3), image = item / (uint32_t)p.nblk;
+        const int blk = (int)(item - image * p.nblk), g0 = blk * p.gpb, ng = min(p.gpb, p.G - g0), c0 = g0 * p.cg, nch = ng * p.cg, cvec = (nch + 7) / 8;
+        const int R = quotient(T, cvec), r = quotient(tid, cvec), at = tid - r * cvec, P = (int)p.P, n = min(8, nch - 8 * at);
+        const bool active = r < R;
+        const X* x = static_cast<const X*>(p.x) + (long long)image * p.P * p.ldx + c0;
+        const norm_lds l(smem, ng, R, cvec);
+        whole_or_not(nch, [&](auto whole) {
+        norm_sums s;
+        s.clear();
+        norm_channels ch;
+        int8_eight<X> v[NV];
+        load_rows<decltype(whole)::value>(v, x, p.ldx, 8 * at, nch, r, R, P);
+        if (active) ch.load(p, c0 + 8 * at, n);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) part[tid * 9 + e] = a[e];
-                __syncthreads();
-                for (int c = tid; c < nch; c += T) {
-                    float s = 0.f;
-                    for (int j = 0; j < R; ++j) s += part[(j * cvec + (c >> 3)) * 9 + (c & 7)];
-                    channel[c] = s;
-                }
-                __syncthreads();
-                for (int g = tid / L; g < ng; g += T / L) {
-                    float s = 0.f;
-                    for (int c = tid % L; c < p.cg; c += L) s += channel[g * p.cg + c];
-                    for (int m = L / 2; m > 0; m >>= 1) s += __shfl_xor(s, m);
-                    if (tid % L == 0) out[g] = s;
-                }
-                __syncthreads();
-            };
-            const float cnt = (float)rows * (float)p.cg;
-            by_group(sum, mean_of);
-            float mean[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) mean[e] = mean_of[min(8 * at + e, nch - 1) / p.cg] / cnt;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+        for (int k = 0; k < NV; ++k)
+            if (active && r + k * R < P) s.add(v[k]);
+        join_threads<T, true>(l, s, at, r, cvec, R, nch, ng, p.cg, p.eps);
+        if (active) {
+            ch.set(p.cg, c0 + 8 * at, n, g0, l.mean, l.m2);
+            const long long row0 = (long long)image * p.P;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
-                if (r + k * R < rows)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float d = v[k].get(e) - mean[e];
-                        sum[e] = fmaf(d, d, sum[e]);
-                    }
-            const float keep = tid < ng ? mean_of[tid] / cnt : 0.f;
-            by_group(sum, mean_of);
-            if (tid < ng) p.parts[(image * p.G + g0 + tid) * p.chunks + chunk] = float4{keep, mean_of[tid], cnt, 0.f};
-            __syncthreads();
+                if (r + k * R < P) {
+                    const long long row = row0 + r + k * R;
+                    float f[8];
+                    ch.apply(v[k], p.act, f);
+                    if (p.token_major) store8(p.y, (size_t)row * p.ldy + c0 + 8 * at, f, n, p.out_bf16);
+                    else store8_apart(p.y, c0 + 8 * at, p.ldy, row, f, n, p.out_bf16);
+                }
         }
+        });
+        __syncthreads();
     }
 }
 
-// The pieces of a group joined: a wavefront for each group of an image.
+// ---- statistics of pieces --------------------------------------------------------------------------------
+// Several groups a workgroup, `rows` positions of them.
+template <typename X>
 __global__ void __launch_bounds__(256)
-norm_join_kernel(const float4* __restrict__ parts, long long groups, long long chunks, float eps, float2* __restrict__ stats) {
-    const int lane = threadIdx.x & 63;
-    for (long long g = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); g < groups; g += (long long)gridDim.x * 4) {
-        const float4* a = parts + g * chunks;
-        double n = 0, s = 0;
-        for (long long c = lane; c < chunks; c += 64) n += a[c].z, s += (double)a[c].z * a[c].x;
-        for (int m = 32; m > 0; m >>= 1) n += __shfl_xor(n, m), s += __shfl_xor(s, m);
-        const double mean = s / n;
-        double m2 = 0;
-        for (long long c = lane; c < chunks; c += 64) {
-            const double d = a[c].x - mean;
-            m2 += a[c].y + a[c].z * d * d;
-        }
-        for (int m = 32; m > 0; m >>= 1) m2 += __shfl_xor(m2, m);
-        if (lane == 0) stats[g] = float2{(float)mean, (float)(1.0 / sqrt(m2 / n + (double)eps))};
+norm_stats_kernel(norm_args p) {
+    constexpr int T = 256;
+    extern __shared__ __align__(16) float smem[];
+    const int tid = threadIdx.x;
+    const uint32_t chunks = (uint32_t)p.chunks, items = (uint32_t)(p.images * p.nblk) * chunks;
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint32_t rest = item / chunks, chunk = item - rest * chunks, image = rest / (uint32_t)p.nblk;
+        const int blk = (int)(rest - image * p.nblk), g0 = blk * p.gpb, ng = min(p.gpb, p.G - g0), c0 = g0 * p.cg, nch = ng * p.cg, cvec = (nch + 7) / 8;
+        const int R = quotient(T, cvec), r = quotient(tid, cvec), at = tid - r * cvec;
+        const long long p0 = (long long)chunk * p.rows;
+        const int rows = (int)min((long long)p.rows, p.P - p0);
+        const bool active = r < R;
+        const X* x = static_cast<const X*>(p.x) + ((long long)image * p.P + p0) * p.ldx + c0;
+        const norm_lds l(smem, ng, R, cvec);
+        norm_sums s;
+        s.clear();
+        if (active) whole_or_not(nch, [&](auto whole) {
+            constexpr int AHEAD = sizeof(X) == 2 ? 8 : 4;
+            for (int pos = r; pos < rows; pos += AHEAD * R) {
+                int8_eight<X> u[AHEAD];
+                load_rows<decltype(whole)::value>(u, x, p.ldx, 8 * at, nch, pos, R, rows);
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k)
+                    if (pos + k * R < rows) s.add(u[k]);
+            }
+        });
+        join_threads<T, false>(l, s, at, r, cvec, R, nch, ng, p.cg, 0.f);
+        for (int g = tid; g < ng; g += T) p.parts[((long long)image * p.G + g0 + g) * p.chunks + chunk] = float4{l.mean[g], l.m2[g], (float)rows * (float)p.cg, 0.f};
+        __syncthreads();
     }
+}
+// One group of many channels: `rows` vectors a thread, of the group's vectors in order, whatever position they belong to.
+template <typename X>
+__global__ void __launch_bounds__(256)
+norm_stats_wide_kernel(norm_args p) {
+    constexpr int T = 256;
+    __shared__ double part[T / 64];
+    const int tid = threadIdx.x, cvec = (p.cg + 7) / 8, step_p = T / cvec, step_v = T % cvec;
+    auto reduce = [&](double a) {
+        for (int m = 32; m > 0; m >>= 1) a += __shfl_xor(a, m);
+        __syncthreads();
+        if ((tid & 63) == 0) part[tid >> 6] = a;
+        __syncthreads();
+        a = 0;
+#pragma unroll
+        for (int w = 0; w < T / 64; ++w) a += part[w];
+        return a;
+    };
+    const uint32_t chunks = (uint32_t)p.chunks, items = (uint32_t)(p.images * p.G) * chunks;
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint32_t group_at = item / chunks, image_at = group_at / (uint32_t)p.G;
+        const long long group = group_at, image = image_at, chunk = item - group_at * chunks;
+        const X* x = static_cast<const X*>(p.x) + image * p.P * p.ldx + (group - image * p.G) * p.cg;
+        const long long first = chunk * T * p.rows + tid;
+        long long pos = first / cvec;
+        int at = (int)(first - pos * cvec), n = 0;
+        float k = 0.f, s1 = 0.f, s2 = 0.f;
+        int8_eight<X> v[MAX_ROWS / 8];
+        int here[MAX_ROWS / 8];
+#pragma unroll
+        for (int i = 0; i < MAX_ROWS / 8; ++i) {
+            here[i] = 0;
+            v[i].zero();
+            if (i >= p.rows) continue;                           // (the same for all)
+            if (pos < p.P) here[i] = min(8, p.cg - 8 * at);
+            if (here[i] == 8) v[i].load(x + pos * p.ldx + 8 * at);
+            else if (here[i]) v[i] = int8_load8(x + pos * p.ldx, 8 * at, p.cg);
+            at += step_v, pos += step_p;
+            if (at >= cvec) at -= cvec, ++pos;
+        }
+#pragma unroll
+        for (int i = 0; i < MAX_ROWS / 8; ++i) {
+            if (i >= p.rows) continue;
+            if (i == 0) k = v[0].get(0);
+            n += here[i];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = e < here[i] ? v[i].get(e) - k : 0.f;
+                s1 += d;
+                s2 = fmaf(d, d, s2);
+            }
+        }
+        const double N = reduce(n), mean = reduce(n ? (double)n * k + s1 : 0.0) / N;
+        double m2 = 0;
+        if (n) {
+            const double d = k + (double)s1 / n - mean;
+            m2 = (double)s2 - (double)s1 * s1 / n + n * d * d;
+        }
+        m2 = reduce(m2);
+        if (tid == 0) p.parts[group * p.chunks + chunk] = float4{(float)mean, (float)m2, (float)N, 0.f};
+    }
+}
+
+// The pieces of groups g0 ... g0 + ng - 1 of an image joined, as above: mean and 1 / sqrt(v + eps).
+template <int T>
+__device__ __forceinline__ void join_parts(const norm_args& p, long long image, int g0, int ng, float* mean, float* rstd) {
+    const int tid = threadIdx.x, chunks = (int)p.chunks, log = lanes_log2(ng, T), L = 1 << log, lane = tid & (L - 1);
+    for (int g = tid >> log; g < ((ng + (T >> log) - 1) & -(T >> log)); g += T >> log) {
+        const float4* a = p.parts + (image * p.G + g0 + min(g, ng - 1)) * p.chunks;
+        double n = 0, sum = 0, sq = 0;
+        auto add = [&](const float4& q) { n += q.z, sum += (double)q.z * q.x, sq += q.y + (double)q.z * q.x * q.x; };
+        int c = lane;
+        for (; c + 3 * L < chunks; c += 4 * L) {
+            const float4 q0 = a[c], q1 = a[c + L], q2 = a[c + 2 * L], q3 = a[c + 3 * L];
+            add(q0), add(q1), add(q2), add(q3);
+        }
+        for (; c < chunks; c += L) add(a[c]);
+        store_joined<true>(n, sum, sq, log, p.eps, g < ng && lane == 0, mean + g, rstd + g);
+    }
+    __syncthreads();
 }
 
 // ---- y ---------------------------------------------------------------------------------------------
-// Token-major: a thread takes eight channels of a position.
-template <typename X>
+// A workgroup has `vecs` vectors of channels and `y_rows` positions of an image.  Token-major: as in the statistics.  Feature-major: lanes along the positions, so
+// that a channel's values leave side by side (x: 16 bytes of a row for each lane, whole lines by the caches).
+template <typename X, bool TOKENS>
 __global__ void __launch_bounds__(256)
-norm_rows_kernel(norm_args p) {
-    const int cvec = (p.C + 7) / 8;
-    const long long total = p.images * p.P * cvec;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const long long row = i / cvec, image = row / p.P;
-        const int c0 = (int)(i - row * cvec) * 8, n = min(8, p.C - c0);
-        const int8_eight<X> v = int8_load8(static_cast<const X*>(p.x) + row * p.ldx, c0, p.C);
+norm_apply_kernel(norm_args p) {
+    constexpr int T = 256;
+    extern __shared__ __align__(16) float smem[];
+    const int tid = threadIdx.x;
+    const uint32_t chunks = (uint32_t)p.y_chunks, items = (uint32_t)(p.images * p.vblk) * chunks;
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        // the pieces read last come first: they are in the caches
+        const uint32_t back = items - 1 - item, rest = back / (uint32_t)p.vblk, blk = back - rest * p.vblk, image_at = rest / chunks;
+        const long long image = image_at, chunk = rest - image_at * chunks;
+        const int c0 = (int)blk * p.vecs * 8, nch = min(p.vecs * 8, p.C - c0), cvec = (nch + 7) / 8, g0 = quotient(c0, p.cg), ng = quotient(c0 + nch - 1, p.cg) - g0 + 1;
+        const long long row0 = image * p.P + chunk * p.y_rows;
+        const int rows = (int)min(p.y_rows, p.P - chunk * p.y_rows);
+        const X* x = static_cast<const X*>(p.x) + row0 * p.ldx + c0;
+        if constexpr (TOKENS) {
+            const int R = quotient(T, cvec), r = quotient(tid, cvec), at = tid - r * cvec, n = min(8, nch - 8 * at);
+            // (the first rows, gamma and beta are on their way while the statistics are joined)
+            whole_or_not(nch, [&](auto whole) {
+                constexpr int AHEAD = sizeof(X) == 2 ? 8 : 4;
+                norm_channels ch;
+                int8_eight<X> u[AHEAD];
+                load_rows<decltype(whole)::value>(u, x, p.ldx, 8 * at, nch, r, R, rows);
+                ch.load(p, c0 + 8 * at, n);
+                join_parts<T>(p, image, g0, ng, smem, smem + ng);
+                if (r >= R) return;
+                ch.set(p.cg, c0 + 8 * at, n, g0, smem, smem + ng);
+                const size_t to = (size_t)row0 * p.ldy + c0 + 8 * at;
+                for (int pos = r; pos < rows; pos += AHEAD * R) {
+                    if (pos != r) load_rows<decltype(whole)::value>(u, x, p.ldx, 8 * at, nch, pos, R, rows);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) {
-                const float2 st = p.stats[image * p.G + (c0 + e) / p.cg];
-                const float h = (v.get(e) - st.x) * (st.y * (p.gamma ? p.gamma[c0 + e] : 1.f)) + (p.beta ? p.beta[c0 + e] : 0.f);
-                tsvd_store_y(p.y, (size_t)row * p.ldy + c0 + e, norm_act(h, p.act), p.out_bf16);
-            }
-    }
-}
-
-// Feature-major: lanes along the positions, so that a channel's values leave side by side; a thread takes eight channels of a position.
-template <typename X>
-__global__ void __launch_bounds__(256)
-norm_columns_kernel(norm_args p) {
-    const int cvec = (p.C + 7) / 8;
-    const long long rows = p.images * p.P, blocks = (rows + 255) / 256, items = blocks * cvec;
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long row = item / cvec * 256 + threadIdx.x;
-        const int c0 = (int)(item % cvec) * 8, n = min(8, p.C - c0);
-        if (row >= rows) continue;
-        const long long image = row / p.P;
-        const int8_eight<X> v = int8_load8(static_cast<const X*>(p.x) + row * p.ldx, c0, p.C);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) {
-                const float2 st = p.stats[image * p.G + (c0 + e) / p.cg];
-                const float h = (v.get(e) - st.x) * (st.y * (p.gamma ? p.gamma[c0 + e] : 1.f)) + (p.beta ? p.beta[c0 + e] : 0.f);
-                tsvd_store_y(p.y, (size_t)(c0 + e) * p.ldy + row, norm_act(h, p.act), p.out_bf16);
-            }
-    }
-}
-
-// Codes: a workgroup for each position, its values computed twice (for the largest magnitude, then for the codes).
-template <typename X>
-__global__ void __launch_bounds__(256)
-norm_int8_kernel(norm_args p) {
-    __shared__ uint32_t lds[4];
-    const int cvec = (p.C + 7) / 8, tid = threadIdx.x;
-    const long long rows = p.images * p.P;
-    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
-        const X* x = static_cast<const X*>(p.x) + row * p.ldx;
-        const float2* stats = p.stats + row / p.P * p.G;
-        auto values = [&](int c0, float (&f)[8]) {
-            const int8_eight<X> v = int8_load8(x, c0, p.C);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                f[e] = 0.f;
-                if (c0 + e < p.C) {
-                    const float2 st = stats[(c0 + e) / p.cg];
-                    f[e] = norm_act((v.get(e) - st.x) * (st.y * (p.gamma ? p.gamma[c0 + e] : 1.f)) + (p.beta ? p.beta[c0 + e] : 0.f), p.act);
+                    for (int k = 0; k < AHEAD; ++k)
+                        if (pos + k * R < rows) {
+                            float f[8];
+                            ch.apply(u[k], p.act, f);
+                            store8(p.y, to + (size_t)(pos + k * R) * p.ldy, f, n, p.out_bf16);
+                        }
+                }
+            });
+        } else {
+            join_parts<T>(p, image, g0, ng, smem, smem + ng);
+            for (int at = 0; at < cvec; ++at) {
+                const int n = min(8, nch - 8 * at);
+                norm_channels ch;
+                ch.load(p, c0 + 8 * at, n);
+                ch.set(p.cg, c0 + 8 * at, n, g0, smem, smem + ng);
+                for (int pos = tid; pos < rows; pos += T) {
+                    float f[8];
+                    ch.apply(int8_load8(x + (long long)pos * p.ldx, 8 * at, nch), p.act, f);
+                    store8_apart(p.y, c0 + 8 * at, p.ldy, row0 + pos, f, n, p.out_bf16);
                 }
             }
-        };
+        }
+        __syncthreads();
+    }
+}
+
+// ---- codes -----------------------------------------------------------------------------------------
+// A wavefront for each position, NV vectors of channels a lane with their factors in registers, `y_rows` positions of an image a workgroup.
+template <typename X, int NV>
+__global__ void __launch_bounds__(256)
+norm_int8_kernel(norm_args p) {
+    extern __shared__ __align__(16) float smem[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cvec = (p.C + 7) / 8;
+    const uint32_t chunks = (uint32_t)p.y_chunks, items = (uint32_t)p.images * chunks;
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint32_t back = items - 1 - item, image_at = back / chunks;
+        const long long image = image_at, first = (back - image_at * chunks) * p.y_rows;
+        const long long row0 = image * p.P + first;
+        const int rows = (int)min(p.y_rows, p.P - first);
+        join_parts<256>(p, image, 0, p.G, smem, smem + p.G);
+        norm_channels ch[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c0 = 8 * (lane + 64 * k);
+            const int n = max(0, min(8, p.C - c0));
+            ch[k].load(p, min(c0, p.C - 1), n);
+            ch[k].set(p.cg, min(c0, p.C - 1), n, 0, smem, smem + p.G);
+        }
+        for (int pos = wave; pos < rows; pos += 4) {
+            const long long row = row0 + pos;
+            float f[NV][8];
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int c0 = 8 * (lane + 64 * k);
+                ch[k].apply(int8_load8(static_cast<const X*>(p.x) + row * p.ldx, c0, p.C), p.act, f[k]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c0 + e < p.C) top = max(top, __float_as_uint(f[k][e]) & 0x7FFFFFFFu);
+            }
+            float scale, factor;
+            int8_factors(int8_wave_top(top), &scale, &factor);
+            if (lane == 0) p.scales[row] = scale;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (lane + 64 * k < cvec) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (size_t)row * p.ldy + 8 * (lane + 64 * k)) = codes_of(f[k], factor);
+        }
+        __syncthreads();
+    }
+}
+// Rows of more channels: a workgroup for each position, the values computed twice (for the largest magnitude, then for the codes).
+template <typename X>
+__global__ void __launch_bounds__(256)
+norm_int8_wide_kernel(norm_args p) {
+    extern __shared__ __align__(16) float smem[];
+    __shared__ uint32_t tops[4];
+    const int tid = threadIdx.x, cvec = (p.C + 7) / 8;
+    const uint32_t chunks = (uint32_t)p.y_chunks, items = (uint32_t)p.images * chunks;
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint32_t image_at = item / chunks;
+        const long long image = image_at, first = (item - image_at * chunks) * p.y_rows;
+        join_parts<256>(p, image, 0, p.G, smem, smem + p.G);
+        for (long long row = image * p.P + first, end = image * p.P + min(p.P, first + p.y_rows); row < end; ++row) {
+            const X* x = static_cast<const X*>(p.x) + row * p.ldx;
+            auto values = [&](int at, float (&f)[8]) {
+                norm_channels ch;
+                ch.load(p, 8 * at, min(8, p.C - 8 * at));
+                ch.set(p.cg, 8 * at, min(8, p.C - 8 * at), 0, smem, smem + p.G);
+                ch.apply(int8_load8(x, 8 * at, p.C), p.act, f);
+            };
+            uint32_t top = 0;
+            for (int at = tid; at < cvec; at += 256) {
+                float f[8];
+                values(at, f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (8 * at + e < p.C) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+            }
+            top = int8_wave_top(top);
+            if ((tid & 63) == 0) tops[tid >> 6] = top;
+            __syncthreads();
+            float scale, factor;
+            int8_factors(max(max(tops[0], tops[1]), max(tops[2], tops[3])), &scale, &factor);
+            if (tid == 0) p.scales[row] = scale;
+            for (int at = tid; at < cvec; at += 256) {
+                float f[8];
+                values(at, f);
+                *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (size_t)row * p.ldy + 8 * at) = codes_of(f, factor);
+            }
+            __syncthreads();
+        }
+        __syncthreads();
+    }
+}
+
+// ---- rows: one position, one group --------------------------------------------------------------------
+// T threads for a row (64: four rows a workgroup), NV vectors of eight channels each, in registers.
+template <typename X, int T, int NV, bool CODES>
+__global__ void __launch_bounds__(T == 64 ? 256 : T)
+norm_rows_kernel(norm_args p) {
+    constexpr int WAVES = T / 64, ROWS = T == 64 ? 4 : 1;
+    __shared__ float sums[2][WAVES];
+    __shared__ uint32_t tops[WAVES];
+    const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, wave = t >> 6, C = p.C;
+    auto reduce = [&](float a, int which) {
+        for (int m = 32; m > 0; m >>= 1) a += __shfl_xor(a, m);
+        if constexpr (T > 64) {
+            if ((t & 63) == 0) sums[which][wave] = a;
+            __syncthreads();
+            a = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) a += sums[which][w];
+        }
+        return a;
+    };
+    for (long long row = (long long)blockIdx.x * ROWS + (T == 64 ? threadIdx.x >> 6 : 0); row < p.images; row += (long long)gridDim.x * ROWS) {
+        const X* x = static_cast<const X*>(p.x) + row * p.ldx;
+        int8_eight<X> v[NV];
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) v[k] = int8_load8(x, 8 * (t + k * T), C);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += v[k].get(e);              // (zeros behind the end)
+        const float mean = reduce(sum, 0) / (float)C;
+        float m2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int n = C - 8 * (t + k * T);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = e < n ? v[k].get(e) - mean : 0.f;
+                m2 = fmaf(d, d, m2);
+            }
+        }
+        const float rstd = 1.f / sqrtf(reduce(m2, 1) / (float)C + p.eps);
         uint32_t top = 0;
-        for (int i = tid; i < cvec; i += 256) {
-            float f[8];
-            values(8 * i, f);
+        float f[CODES ? NV : 1][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
-        }
-        top = int8_wave_top(top);
-        __syncthreads();
-        if ((tid & 63) == 0) lds[tid >> 6] = top;
-        __syncthreads();
-        top = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
-        float scale, factor;
-        int8_factors(top, &scale, &factor);
-        if (tid == 0) p.scales[row] = scale;
-        for (int i = tid; i < cvec; i += 256) {
-            float f[8];
-            values(8 * i, f);
-            uint32_t c[8];
+        for (int k = 0; k < NV; ++k) {
+            const int c0 = 8 * (t + k * T), n = C - c0;
+            float(&h)[8] = f[CODES ? k : 0];
+            norm_channels ch;
+            if (n > 0) {
+                ch.load(p, c0, n);
+                ch.set(mean, rstd);
+                ch.apply(v[k], p.act, h);
+                if constexpr (CODES) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) c[e] = int8_code(f[e], factor);
-            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (size_t)row * p.ldy + 8 * i) = uint2{int8_pack4(c[0], c[1], c[2], c[3]), int8_pack4(c[4], c[5], c[6], c[7])};
+                    for (int e = 0; e < 8; ++e)
+                        if (e < n) top = max(top, __float_as_uint(h[e]) & 0x7FFFFFFFu);
+                } else {
+                    if (p.token_major) store8(p.y, (size_t)row * p.ldy + c0, h, n, p.out_bf16);
+                    else store8_apart(p.y, c0, p.ldy, row, h, n, p.out_bf16);
+                }
+            }
         }
+        if constexpr (CODES) {
+            top = int8_wave_top(top);
+            if constexpr (T > 64) {
+                if ((t & 63) == 0) tops[wave] = top;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
+            }
+            float scale, factor;
+            int8_factors(top, &scale, &factor);
+            if (t == 0) p.scales[row] = scale;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (8 * (t + k * T) < C) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (size_t)row * p.ldy + 8 * (t + k * T)) = codes_of(f[k], factor);
+        }
+        if constexpr (T > 64) __syncthreads();
     }
 }
 
 // ---- the calls -------------------------------------------------------------------------------------
 size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
 unsigned grid_of(long long blocks) { return (unsigned)std::min<long long>(blocks, 1 << 20); }
+long long up(long long v, long long m) { return (v + m - 1) / m; }
 
-constexpr int STATS_T = 256, STATS_NV = 8;
+constexpr int CUS = 256, VECS = 20, MAX_GROUPS = 4096;
 
-// How the channels and positions of an image are cut for the statistics: about 64 channels (128 bytes of bf16, a line) of whole groups a workgroup, one group where it has more.
-void cut(long long P, int C, int G, norm_args* a) {
-    a->C = C, a->G = G, a->cg = C / G, a->P = P;
-    a->gpb = std::max(1, std::min(G, 64 / a->cg));
-    a->nblk = (G + a->gpb - 1) / a->gpb;
-    if (a->gpb == 1) {
-        a->rows = 0;
-        a->chunks = (P * ((a->cg + 7) / 8) + STATS_T * STATS_NV - 1) / (STATS_T * STATS_NV);
-    } else {
-        const int cvec = (a->gpb * a->cg + 7) / 8;
-        a->rows = STATS_T / cvec * STATS_NV;
-        a->chunks = (P + a->rows - 1) / a->rows;
-    }
+// Groups whose channels are whole vectors, where that takes 128 channels at most.
+int whole_groups(int cg) {
+    int unit = 1;
+    while (unit < 8 && unit * cg % 8 != 0) unit *= 2;
+    return unit * cg % 8 == 0 && unit * cg <= 128 ? unit : 1;
 }
-size_t stats_bytes(long long images, int G) { return round256((size_t)images * G * sizeof(float2)); }
+// Statistics by pieces: whole groups of about 160 channels side by side (whole lines of x; each workgroup that makes y reads all pieces of its groups, so few groups and few
+// pieces: 32 groups by 64 pieces took as long as the rows themselves), pieces of up to 64 positions a thread, about 512 workgroups in all where x is small.
+void cut(long long images, long long P, int C, int G, norm_args* a) {
+    a->images = images, a->P = P, a->C = C, a->G = G, a->cg = C / G;
+    a->gpb = std::min(G, VECS * 8 / a->cg);
+    if (a->gpb <= 1 && a->cg > 64) {
+        a->gpb = 0;                                          // one group, by its vectors
+        a->nblk = G;
+        const long long vecs = P * up(a->cg, 8);
+        a->rows = (int)std::max<long long>(1, std::min<long long>(MAX_ROWS / 8, up(vecs * images * G, 1024 * 256)));
+        a->chunks = up(vecs, 256 * a->rows);
+        return;
+    }
+    a->nblk = (int)up(G, a->gpb);
+    const int unit = whole_groups(a->cg);
+    a->gpb = (int)(up(up(G, a->nblk), unit) * unit);
+    a->nblk = (int)up(G, a->gpb);
+    const int R = 256 / (int)up(a->gpb * a->cg, 8);
+    const long long per = std::max<long long>(1, std::min<long long>(MAX_ROWS, up(images * a->nblk * P, 512 * R)));
+    a->rows = (int)std::min<long long>(per * R, P);
+    a->chunks = up(P, a->rows);
+}
+// y: vectors and positions of a workgroup: up to 16 positions a thread, about 1024 workgroups in all where x is small.
+void cut_y(norm_args* a, bool token_major) {
+    const int cvec = (int)up(a->C, 8);
+    if (token_major) {
+        a->vblk = (int)up(cvec, VECS);
+        a->vecs = (int)up(cvec, a->vblk);
+        const int R = 256 / a->vecs;
+        a->y_rows = std::min<long long>(a->P, R * std::max<long long>(1, std::min<long long>(16, up(a->images * a->vblk * a->P, 1024 * R))));
+    } else {
+        a->vecs = std::min(cvec, 16);
+        a->vblk = (int)up(cvec, a->vecs);
+        a->y_rows = std::min<long long>(a->P, 256);
+    }
+    a->y_chunks = up(a->P, a->y_rows);
+}
 
+// One launch: the groups of a workgroup, 0 where it would hold too much.  64 bytes of a row at least if that still gives every compute unit a workgroup.
 template <typename X>
-hipError_t statistics(const norm_args& a, hipStream_t stream) {
-    const dim3 grid(grid_of(a.images * a.nblk * a.chunks));
-    if (a.gpb == 1) hipLaunchKernelGGL((norm_stats_kernel<X, STATS_T, STATS_NV, true>), grid, dim3(STATS_T), 0, stream, a);
-    else hipLaunchKernelGGL((norm_stats_kernel<X, STATS_T, STATS_NV, false>), grid, dim3(STATS_T), 0, stream, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const long long groups = a.images * a.G;
-    hipLaunchKernelGGL(norm_join_kernel, dim3(grid_of((groups + 3) / 4)), dim3(256), 0, stream, a.parts, groups, a.chunks, a.eps, a.stats);
+int one_launch(const norm_args& a, int T, int rows_of_thread) {
+    int gpb = std::min(a.G, T * 8 / a.cg);
+    if (gpb < 1) return 0;
+    // whole vectors side by side where groups allow it
+    const int unit = whole_groups(a.cg) <= gpb ? whole_groups(a.cg) : 1;
+    while (gpb > unit && (a.images * up(a.G, gpb) < CUS || up(a.P, T / up((long long)gpb * a.cg, 8)) > rows_of_thread) &&
+           (long long)std::max(unit, gpb / 2 / unit * unit) * a.cg * (int)sizeof(X) >= 64) gpb = std::max(unit, gpb / 2 / unit * unit);
+    return up(a.P, T / up((long long)gpb * a.cg, 8)) <= rows_of_thread ? gpb : 0;
+}
+
+template <typename K>
+hipError_t launch(K kernel, long long items, int T, size_t lds, hipStream_t stream, const norm_args& a) {
+    if (items > INT32_MAX) return hipErrorNotSupported;      // (kernels count in 32 bits)
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3(grid_of(items)), dim3(T), lds, stream, a);
     return hipGetLastError();
 }
 
+template <typename X, bool CODES>
+hipError_t rows_form(const norm_args& a, hipStream_t stream) {
+    if (a.C <= 512) return launch(norm_rows_kernel<X, 64, 1, CODES>, up(a.images, 4), 256, 0, stream, a);
+    if (a.C <= 1024) return launch(norm_rows_kernel<X, 64, 2, CODES>, up(a.images, 4), 256, 0, stream, a);
+    if (a.C <= 2048) return launch(norm_rows_kernel<X, 256, 1, CODES>, a.images, 256, 0, stream, a);
+    if (a.C <= 4096) return launch(norm_rows_kernel<X, 256, 2, CODES>, a.images, 256, 0, stream, a);
+    if (a.C <= 8192) return launch(norm_rows_kernel<X, 256, 4, CODES>, a.images, 256, 0, stream, a);
+    return launch(norm_rows_kernel<X, 1024, 2, CODES>, a.images, 1024, 0, stream, a);
+}
+
+template <typename X>
+hipError_t statistics(const norm_args& a, hipStream_t stream) {
+    if (a.gpb == 0) return launch(norm_stats_wide_kernel<X>, a.images * a.G * a.chunks, 256, 0, stream, a);
+    const int cvec = (int)up((long long)a.gpb * a.cg, 8);
+    return launch(norm_stats_kernel<X>, a.images * a.nblk * a.chunks, 256, norm_lds::bytes(a.gpb, 256 / cvec, cvec), stream, a);
+}
+
+template <typename X>
+hipError_t norm(norm_args a, hipStream_t stream) {
+    if (a.P == 1 && a.G == 1 && a.C <= 16384) return rows_form<X, false>(a, stream);
+    for (int T : {256, 512}) {
+        const int gpb = one_launch<X>(a, T, T == 256 ? 8 : 16);
+        if (!gpb) continue;
+        norm_args b = a;
+        b.gpb = gpb, b.nblk = (int)up(a.G, gpb);
+        const int cvec = (int)up((long long)gpb * a.cg, 8);
+        const size_t lds = norm_lds::bytes(gpb, T / cvec, cvec);
+        return T == 256 ? launch(norm_one_kernel<X, 256, 8>, b.images * b.nblk, T, lds, stream, b) : launch(norm_one_kernel<X, 512, 16>, b.images * b.nblk, T, lds, stream, b);
+    }
+    const hipError_t e = statistics<X>(a, stream);
+    if (e != hipSuccess) return e;
+    cut_y(&a, a.token_major);
+    const long long items = a.images * a.vblk * a.y_chunks;
+    const size_t lds = 8 * ((size_t)std::min<long long>(a.G, a.vecs * 8) + 1);
+    return a.token_major ? launch(norm_apply_kernel<X, true>, items, 256, lds, stream, a) : launch(norm_apply_kernel<X, false>, items, 256, lds, stream, a);
+}
+template <typename X>
+hipError_t norm_codes(norm_args a, hipStream_t stream) {
+    if (a.P == 1 && a.G == 1 && a.C <= 16384) return rows_form<X, true>(a, stream);
+    const hipError_t e = statistics<X>(a, stream);
+    if (e != hipSuccess) return e;
+    a.y_rows = std::min<long long>(a.P, 4 * std::max<long long>(4, std::min<long long>(MAX_ROWS, up(a.images * a.P, 2048 * 4))));
+    a.y_chunks = up(a.P, a.y_rows);
+    const size_t lds = 8 * (size_t)a.G;
+    if (a.C <= 512) return launch(norm_int8_kernel<X, 1>, a.images * a.y_chunks, 256, lds, stream, a);
+    if (a.C <= 1024) return launch(norm_int8_kernel<X, 2>, a.images * a.y_chunks, 256, lds, stream, a);
+    a.y_rows = std::min<long long>(a.P, 4);
+    a.y_chunks = up(a.P, a.y_rows);
+    return launch(norm_int8_wide_kernel<X>, a.images * a.y_chunks, 256, lds, stream, a);
+}
+
+tsvd_status status_of(hipError_t e) { return e == hipSuccess ? TSVD_OK : e == hipErrorNotSupported ? TSVD_EUNSUPPORTED : TSVD_EDEVICE; }
 bool bad_dtype(int t) { return t != TSVD_F32 && t != TSVD_BF16; }
 
 tsvd_status common(const void* x, tsvd_dtype x_dtype, int64_t images, int64_t P, int64_t C, int64_t ldx, int64_t groups, const float* gamma, const float* beta, float eps,
@@ -318,23 +792,22 @@ tsvd_status common(const void* x, tsvd_dtype x_dtype, int64_t images, int64_t P,
     if (!x || images < 1 || P < 1 || C < 1 || groups < 1 || bad_dtype(x_dtype) || ldx < C || !(eps > 0.f) || !std::isfinite(eps) || act < TSVD_ACT_NONE || act > TSVD_ACT_GELU)
         return TSVD_EINVAL;
     if (C % groups != 0) return TSVD_EINVAL;
-    if (C > (1 << 20) || images > INT32_MAX / P) return TSVD_EUNSUPPORTED;
+    if (C > (1 << 20) || groups > MAX_GROUPS || images > INT32_MAX / P) return TSVD_EUNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < tsvd_group_norm_workspace_bytes(images, P, C, groups)) return TSVD_EINVAL;
-    a->x = x, a->ldx = ldx, a->images = images;
+    a->x = x, a->ldx = ldx;
     a->gamma = gamma, a->beta = beta, a->eps = eps, a->act = act;
-    cut(P, (int)C, (int)groups, a);
-    a->stats = static_cast<float2*>(workspace);
-    a->parts = reinterpret_cast<float4*>(static_cast<uint8_t*>(workspace) + stats_bytes(images, (int)groups));
+    cut(images, P, (int)C, (int)groups, a);
+    a->parts = static_cast<float4*>(workspace);
     return TSVD_OK;
 }
 
 }  // namespace
 
 extern "C" size_t tsvd_group_norm_workspace_bytes(int64_t images, int64_t positions, int64_t C, int64_t groups) {
-    if (images < 1 || positions < 1 || C < 1 || groups < 1 || C % groups != 0 || C > (1 << 20) || images > INT32_MAX / positions) return 0;
+    if (images < 1 || positions < 1 || C < 1 || groups < 1 || C % groups != 0 || C > (1 << 20) || groups > MAX_GROUPS || images > INT32_MAX / positions) return 0;
     norm_args a = {};
-    cut(positions, (int)C, (int)groups, &a);
-    return stats_bytes(images, (int)groups) + round256((size_t)images * groups * a.chunks * sizeof(float4));
+    cut(images, positions, (int)C, (int)groups, &a);
+    return round256((size_t)images * groups * a.chunks * sizeof(float4));
 }
 
 extern "C" tsvd_status tsvd_group_norm(const void* x_dev, tsvd_dtype x_dtype, int64_t images, int64_t positions, int64_t C, int64_t ldx, int64_t groups,
@@ -345,21 +818,9 @@ extern "C" tsvd_status tsvd_group_norm(const void* x_dev, tsvd_dtype x_dtype, in
     const tsvd_status st = common(x_dev, x_dtype, images, positions, C, ldx, groups, gamma_dev, beta_dev, eps, act, workspace, workspace_bytes, &a);
     if (st != TSVD_OK) return st;
     if (ldy < (y_layout == TSVD_TOKEN_MAJOR ? C : images * positions)) return TSVD_EINVAL;
-    a.y = y_dev, a.ldy = ldy, a.out_bf16 = y_dtype == TSVD_BF16;
+    a.y = y_dev, a.ldy = ldy, a.out_bf16 = y_dtype == TSVD_BF16, a.token_major = y_layout == TSVD_TOKEN_MAJOR;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = x_dtype == TSVD_BF16 ? statistics<uint16_t>(a, s) : statistics<float>(a, s);
-    if (e != hipSuccess) return TSVD_EDEVICE;
-    const long long rows = a.images * a.P, cvec = (C + 7) / 8;
-    if (y_layout == TSVD_TOKEN_MAJOR) {
-        const dim3 grid(grid_of((rows * cvec + 255) / 256));
-        if (x_dtype == TSVD_BF16) hipLaunchKernelGGL(norm_rows_kernel<uint16_t>, grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL(norm_rows_kernel<float>, grid, dim3(256), 0, s, a);
-    } else {
-        const dim3 grid(grid_of((rows + 255) / 256 * cvec));
-        if (x_dtype == TSVD_BF16) hipLaunchKernelGGL(norm_columns_kernel<uint16_t>, grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL(norm_columns_kernel<float>, grid, dim3(256), 0, s, a);
-    }
-    return hipGetLastError() == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
+    return status_of(x_dtype == TSVD_BF16 ? norm<uint16_t>(a, s) : norm<float>(a, s));
 }
 
 extern "C" tsvd_status tsvd_group_norm_int8(const void* x_dev, tsvd_dtype x_dtype, int64_t images, int64_t positions, int64_t C, int64_t ldx, int64_t groups,
@@ -373,10 +834,5 @@ extern "C" tsvd_status tsvd_group_norm_int8(const void* x_dev, tsvd_dtype x_dtyp
     if (C > TSVD_INT8_MAX_N) return TSVD_EUNSUPPORTED;
     a.y = codes_dev, a.ldy = ldq, a.scales = scales_dev;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = x_dtype == TSVD_BF16 ? statistics<uint16_t>(a, s) : statistics<float>(a, s);
-    if (e != hipSuccess) return TSVD_EDEVICE;
-    const dim3 grid(grid_of(a.images * a.P));
-    if (x_dtype == TSVD_BF16) hipLaunchKernelGGL(norm_int8_kernel<uint16_t>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(norm_int8_kernel<float>, grid, dim3(256), 0, s, a);
-    return hipGetLastError() == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
+    return status_of(x_dtype == TSVD_BF16 ? norm_codes<uint16_t>(a, s) : norm_codes<float>(a, s));
 }

@@ -37,6 +37,7 @@ struct tsvd_int8_problem {
     long long ldy;
 };
 hipError_t tsvd_int8_gemm(const tsvd_int8_problem& p, hipStream_t stream);       // tsvd_int8_gemm.hip: any number of tokens
+hipError_t tsvd_int8_gemm_init();                                                // once for each device
 // tsvd_int8_stream.hip: few tokens; and from rows of x, where it makes the codes itself (p.codes and p.scales are not used then)
 bool tsvd_int8_stream_serves(const tsvd_int8_handle& h, long long B);
 hipError_t tsvd_int8_stream(const tsvd_int8_problem& p, hipStream_t stream);

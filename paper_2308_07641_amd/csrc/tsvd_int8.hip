@@ -212,6 +212,10 @@ extern "C" tsvd_status tsvd_int8_pack(const int8_t* w_dev, int64_t ldw, const fl
         (void)hipGetLastError();
         return TSVD_EDEVICE;
     }
+    if (tsvd_int8_gemm_init() != hipSuccess) {
+        (void)hipGetLastError();
+        return TSVD_EDEVICE;
+    }
     tsvd_int8_handle* h = new (std::nothrow) tsvd_int8_handle();
     if (!h) return TSVD_ENOMEM;
     h->device = device;
@@ -262,7 +266,7 @@ extern "C" tsvd_status tsvd_int8_product(const tsvd_int8_handle* h, const int8_t
     if (B > TSVD_INT8_MAX_B || ldq > TSVD_INT8_MAX_PITCH) return TSVD_EUNSUPPORTED;
     const tsvd_int8_problem p = {h, codes_dev, ldq, scales_dev, B, bias_dev, y_dev, y_dtype == TSVD_BF16, y_layout == TSVD_TOKEN_MAJOR, ldy};
     const hipError_t e = tsvd_int8_stream_serves(*h, B) ? tsvd_int8_stream(p, static_cast<hipStream_t>(stream)) : tsvd_int8_gemm(p, static_cast<hipStream_t>(stream));
-    return e == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
+    return e == hipSuccess ? TSVD_OK : e == hipErrorNotSupported ? TSVD_EUNSUPPORTED : TSVD_EDEVICE;
 }
 
 extern "C" size_t tsvd_int8_workspace_bytes(const tsvd_int8_handle* h, int64_t B, tsvd_dtype x_dtype, tsvd_layout x_layout) {

@@ -142,6 +142,8 @@ int8_stream_kernel(stream_args p) {
     }
 }
 
+constexpr int MAX_BLOCKS = 48;      // 60 KiB of sums
+
 // How a launch is laid out: strips of a workgroup (all workgroups at once on the compute units, sums within 64 KiB of LDS), wavefronts and tiles of each.
 struct stream_plan {
     int strips_wg, kw, sw, kt, nb;
@@ -149,7 +151,7 @@ struct stream_plan {
 stream_plan plan_of(long long strips, int nkt, long long B, int cus, int most) {
     stream_plan s;
     s.nb = B <= 16 ? 1 : B <= 32 ? 2 : 4;
-    s.strips_wg = (int)std::max<long long>(1, std::min<long long>((strips + cus - 1) / cus, 48 / s.nb));
+    s.strips_wg = (int)std::max<long long>(1, std::min<long long>((strips + cus - 1) / cus, MAX_BLOCKS / s.nb));
     s.kt = std::min(most, s.nb == 1 ? 8 : 4);
     s.kw = 1;
     while (s.kw < 16 && s.kw * s.kt < nkt) s.kw *= 2;
@@ -163,11 +165,7 @@ stream_plan plan_of(long long strips, int nkt, long long B, int cus, int most) {
 
 template <int KT, int NB, typename MAKE>
 hipError_t launch(const stream_args& a, int grid, hipStream_t stream) {
-    const size_t lds = (size_t)a.strips_wg * NB * BLOCK * 4;
-    if (lds > 48 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(int8_stream_kernel<KT, NB, MAKE>), hipFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
-        if (e != hipSuccess) return e;
-    }
+    const size_t lds = (size_t)a.strips_wg * NB * BLOCK * 4;          // (within the 64 KiB that need no permission: plan_of)
     hipLaunchKernelGGL((int8_stream_kernel<KT, NB, MAKE>), dim3(grid), dim3(64 * a.kw * a.sw), lds, stream, a);
     return hipGetLastError();
 }

@@ -155,6 +155,36 @@ def test_layer_against_64_bits(tsvd, M, N, B):
     tsvd.tsvd_int8_free(h)
 
 
+@pytest.mark.parametrize("tile", [1, 2, 3, 4])
+@pytest.mark.parametrize("M,N,B", [(64, 128, 65), (65, 64, 66), (257, 385, 130), (300, 1000, 257), (1000, 2049, 100), (513, 130, 600), (37, 4100, 71)])
+def test_every_tile_gives_the_same_bits(tsvd, M, N, B, tile):
+    """Every kind of tile, ragged in all three sizes (stages 1 to 33, odd and even), both layouts and types, against 64 bits; the sums are whole numbers and the
+    rest the same three roundings, so the kinds agree bit for bit."""
+    import torch
+    rng = np.random.default_rng(M + N + B)
+    w, t, bias = layer(rng, M, N)
+    h = packed(tsvd, w, t)
+    x, ref = gpu_x(values(rng, B, N), "bf16", True)
+    q, s = tsvd.tsvd_int8_quantize(x)
+    b = torch.from_numpy(bias).to("cuda:0")
+    want, p = plain_layer(*plain_codes(ref), w.astype(np.float64), t, bias)
+    for y_tm in (True, False):
+        for y_bf16 in (True, False):
+            print(f"case tile {tile} {M} {N} {B} y_tm={y_tm} bf16={y_bf16}", flush=True)
+            kw = dict(bias=b, y_dtype=tsvd.TSVD_BF16 if y_bf16 else tsvd.TSVD_F32, y_layout=tsvd.TSVD_TOKEN_MAJOR if y_tm else tsvd.TSVD_FEATURE_MAJOR)
+            tsvd.tsvd_tuning_set("TSVD_INT8_TILE", tile)
+            rows, cols = (B, M) if y_tm else (M, B)
+            full = torch.full((rows + 1, cols + 3), 7.0, dtype=torch.bfloat16 if y_bf16 else torch.float32, device="cuda:0")
+            y = tsvd.tsvd_int8_product(h, q, s, y=full[:rows, :cols], **kw)
+            tsvd.tsvd_tuning_reset()
+            assert bool((full[rows:] == 7).all()) and bool((full[:, cols:] == 7).all())
+            v = y.double().cpu().numpy()
+            v = v if y_tm else v.T
+            assert np.all(np.abs(v - want) <= allowed(want, p, y_bf16))
+            assert torch.equal(y, tsvd.tsvd_int8_product(h, q, s, **kw))
+    tsvd.tsvd_int8_free(h)
+
+
 def test_largest_sums_are_exact(tsvd):
     """All codes at their ends: the sum reaches 2^31 - 2^14 and stays a whole number."""
     import torch

@@ -41,7 +41,7 @@ extern "C" {
  *   second copy of U in the five-elements-per-byte code and run stage U of single-token calls on it),
  *   TSVD_EARLY_TILES (0: the single-token kernels request their first weight tile only after the activations are in),
  *   TSVD_TRANSITION_SHIFTED (squarings of a transition's shifted pairs, whatever those before needed),
- *   TSVD_INT8_TILE (1 .. 4: tiles of 64 x 64, 128 x 64, 128 x 128, 256 x 256 rows x tokens for products of 8-bit codes of more than 64 tokens).
+ *   TSVD_INT8_TILE (1 .. 5: tiles of 64 x 64, 128 x 64, 128 x 128, 256 x 128, 256 x 256 rows x tokens for products of 8-bit codes of more than 64 tokens).
  * Returns 0, or 1 for an unknown name. */
 int tsvd_tuning_set(const char* name, int value);
 

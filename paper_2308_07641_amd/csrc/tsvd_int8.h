@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "../../include/tsvd_int8.h"
+#include "tsvd_wave.h"
 
 // Packed weights: scales [strips * 16] fp32 (rounded up to 256 bytes), then tiles of 16 rows x 64 columns of codes, 1 KiB each: lane l of a
 // wavefront finds row l % 16, columns 16 (l / 16) ... + 15, the operand of v_mfma_i32_16x16x64_i8.  A strip's tiles are contiguous along the
@@ -75,6 +76,11 @@ struct int8_eight<uint16_t> {
     __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const vec_at*>(p); }
     __device__ __forceinline__ void set(int e, uint16_t x) { v[e >> 1] |= (uint32_t)x << (16 * (e & 1)); }
     __device__ __forceinline__ float get(int e) const { return __uint_as_float(e & 1 ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16); }
+    // the values from number `by` on, zeros behind them (0 <= by <= 8)
+    __device__ __forceinline__ void shift(int by) {
+        typedef unsigned __int128 u128;
+        v = by < 8 ? __builtin_bit_cast(vec, __builtin_bit_cast(u128, v) >> (16 * by)) : vec{0, 0, 0, 0};
+    }
 };
 template <>
 struct int8_eight<float> {
@@ -88,13 +94,25 @@ struct int8_eight<float> {
     }
     __device__ __forceinline__ void set(int e, float x) { if (e < 4) a[e] = x; else b[e - 4] = x; }
     __device__ __forceinline__ float get(int e) const { return e < 4 ? a[e] : b[e - 4]; }
+    __device__ __forceinline__ void shift(int by) {
+        float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+#pragma unroll
+        for (int s = 1; s <= 8; s *= 2)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = by & s ? (e + s < 8 ? x[e + s] : 0.f) : x[e];
+        a = vec{x[0], x[1], x[2], x[3]};
+        b = vec{x[4], x[5], x[6], x[7]};
+    }
 };
-// Values at .. at + 7 of a row of n, zeros behind its end.
+// Values at .. at + 7 of a row of n, zeros behind its end.  The last ones are read to end at its end and shifted: one load as elsewhere, where a value at a time would be
+// seven, one behind the other.
 template <typename X>
 __device__ __forceinline__ int8_eight<X> int8_load8(const X* row, int at, int n) {
     int8_eight<X> r;
-    if (at + 8 <= n) {
-        r.load(row + at);
+    if (n >= 8) {                                                // (the same for all lanes of a call's launch, nearly always)
+        const int from = min(at, n - 8);
+        r.load(row + from);
+        if (at > from) r.shift(min(at - from, 8));
     } else {
         r.zero();
 #pragma unroll
@@ -116,10 +134,15 @@ __device__ __forceinline__ uint2 int8_codes8(const int8_eight<X>& r, float facto
     for (int e = 0; e < 8; ++e) c[e] = int8_code(r.get(e), factor);
     return uint2{int8_pack4(c[0], c[1], c[2], c[3]), int8_pack4(c[4], c[5], c[6], c[7])};
 }
-__device__ __forceinline__ uint32_t int8_wave_top(uint32_t v) {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, m));
-    return v;
+// The largest over T neighbouring lanes, in all of them.
+template <int T>
+__device__ __forceinline__ uint32_t int8_lanes_top(uint32_t v) {
+    if constexpr (T > 32) v = max(v, lane_xor32<32>(v));
+    if constexpr (T > 16) v = max(v, lane_xor32<16>(v));
+    if constexpr (T > 8) v = max(v, lane_xor32<8>(v));
+    if constexpr (T > 4) v = max(v, lane_xor32<4>(v));
+    if constexpr (T > 2) v = max(v, lane_xor32<2>(v));
+    return max(v, lane_xor32<1>(v));
 }
 
 }  // namespace

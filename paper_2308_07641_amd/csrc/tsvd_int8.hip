@@ -16,31 +16,33 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
 long long round_up(long long v, long long m) { return (v + m - 1) / m * m; }
 
-// The largest over the workgroup's wavefronts.
+// The largest over T threads: some lanes of a wavefront, or a workgroup's wavefronts.
 template <int T>
-__device__ __forceinline__ uint32_t workgroup_top(uint32_t top, uint32_t* lds) {
-    top = int8_wave_top(top);
-    if constexpr (T > 64) {
+__device__ __forceinline__ uint32_t group_top(uint32_t top, uint32_t* lds) {
+    if constexpr (T <= 64) {
+        return int8_lanes_top<T>(top);
+    } else {
         const int wave = threadIdx.x >> 6;
+        top = int8_lanes_top<64>(top);
         if ((threadIdx.x & 63) == 0) lds[wave] = top;
         __syncthreads();
         top = 0;
 #pragma unroll
         for (int w = 0; w < T / 64; ++w) top = max(top, lds[w]);
         __syncthreads();
+        return top;
     }
-    return top;
 }
 
-// Token-major x.  T threads for a token, NV vectors of eight values each, which stay in registers between the largest magnitude and the codes; NV = 0: a loop, x
-// read twice (the second time from the caches).  T = 64: four tokens a workgroup.
+// Token-major x.  T threads for a token (T < 256: several tokens a workgroup), NV vectors of eight values each, which stay in registers between the largest magnitude
+// and the codes; NV = 0: a loop, x read twice (the second time from the caches).
 template <typename X, int T, int NV>
-__global__ void __launch_bounds__(T == 64 ? 256 : T)
+__global__ void __launch_bounds__(T < 256 ? 256 : T)
 int8_quantize_rows_kernel(const X* __restrict__ x, long long ldx, long long B, int N, uint8_t* __restrict__ q, long long ldq, float* __restrict__ s) {
-    __shared__ uint32_t lds[T / 64];
-    constexpr int TOKENS = T == 64 ? 4 : 1;
-    const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, nvec = (N + 7) / 8;
-    for (long long b = (long long)blockIdx.x * TOKENS + (T == 64 ? threadIdx.x >> 6 : 0); b < B; b += (long long)gridDim.x * TOKENS) {
+    __shared__ uint32_t lds[T < 64 ? 1 : T / 64];
+    constexpr int TOKENS = T < 256 ? 256 / T : 1;
+    const int t = threadIdx.x % T, nvec = (N + 7) / 8;
+    for (long long b = (long long)blockIdx.x * TOKENS + threadIdx.x / T; b < B; b += (long long)gridDim.x * TOKENS) {
         const X* row = x + b * ldx;
         uint8_t* out = q + b * ldq;
         uint32_t top = 0;
@@ -51,40 +53,68 @@ int8_quantize_rows_kernel(const X* __restrict__ x, long long ldx, long long B, i
             for (int k = 0; k < NV; ++k) r[k] = int8_load8(row, (t + k * T) * 8, N);
 #pragma unroll
             for (int k = 0; k < NV; ++k) top = int8_top8(r[k], top);
-            int8_factors(workgroup_top<T>(top, lds), &scale, &factor);
+            int8_factors(group_top<T>(top, lds), &scale, &factor);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
                 if (t + k * T < nvec) *reinterpret_cast<uint2*>(out + (size_t)(t + k * T) * 8) = int8_codes8(r[k], factor);
         } else {
             for (int v = t; v < nvec; v += T) top = int8_top8(int8_load8(row, v * 8, N), top);
-            int8_factors(workgroup_top<T>(top, lds), &scale, &factor);
+            int8_factors(group_top<T>(top, lds), &scale, &factor);
             for (int v = t; v < nvec; v += T) *reinterpret_cast<uint2*>(out + (size_t)v * 8) = int8_codes8(int8_load8(row, v * 8, N), factor);
         }
         if (t == 0) s[b] = scale;
     }
 }
 
-// Feature-major x [N][B]: a workgroup takes 8 TV tokens.  A thread loads eight tokens of a row of x at a time; the largest magnitudes of the tokens meet in
-// LDS, then x is read again (from the caches), four rows a thread, and the codes pass through LDS so that a token's bytes leave side by side.
-template <typename X, int TV>
-__global__ void __launch_bounds__(256)
+// Feature-major x [N][B]: a workgroup of T threads takes 8 TV tokens.  A thread loads eight tokens of a row of x at a time, four rows in a pass; the largest magnitudes of the tokens meet in
+// LDS; then the codes of a pass go through LDS, so that a token's bytes leave side by side.  PASSES: x stays in registers in between (N <= PASSES 4 T / TV); 0: it is read again (from the
+// caches).
+template <typename X, int T, int TV, int PASSES>
+__global__ void __launch_bounds__(T, T == 1024 && PASSES <= 2 && TV > 1 && sizeof(X) == 2 ? 8 : 1)
 int8_quantize_columns_kernel(const X* __restrict__ x, long long ldx, long long B, int N, uint8_t* __restrict__ q, long long ldq, float* __restrict__ s) {
-    constexpr int ROWS = 256 / TV, STEP = 4 * ROWS, PITCH = STEP + 16, TOKENS = 8 * TV;      // rows of threads; features a pass
+    constexpr int ROWS = T / TV, STEP = 4 * ROWS, PITCH = STEP + 16, TOKENS = 8 * TV;        // rows of threads; features a pass
     __shared__ uint32_t tops[TOKENS];
     __shared__ __align__(16) uint8_t tile[TOKENS * PITCH];
     const int v = threadIdx.x % TV, r = threadIdx.x / TV;
-    const long long b0 = (long long)blockIdx.x * TOKENS;
+    // workgroups go round the XCDs: neighbours, which share lines of x, are to meet in one L2
+    const unsigned each = gridDim.x >> 3, more = gridDim.x & 7, xcd = blockIdx.x & 7;
+    const long long b0 = (long long)(xcd * each + min(xcd, more) + (blockIdx.x >> 3)) * TOKENS;
     const int tokens = (int)min((long long)TOKENS, B - b0);
     if (threadIdx.x < TOKENS) tops[threadIdx.x] = 0;
-    __syncthreads();
+    const X* mine = x + b0;
+    const int at = min(8 * v, tokens - 1);                       // (beyond the last token: that one's again, not stored)
+    auto load = [&](int8_eight<X> (&u)[4], int n) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = int8_load8(mine + (size_t)min(n + j, N - 1) * ldx, at, tokens);
+    };
     uint32_t top[8] = {};
-    for (int n = r; n < N; n += ROWS) {
-        const int8_eight<X> e = int8_load8(x + (size_t)n * ldx + b0, 8 * v, tokens);
+    auto raise = [&](const int8_eight<X> (&u)[4]) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) top[k] = max(top[k], __float_as_uint(e.get(k)) & 0x7FFFFFFFu);
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top[k] = max(top[k], __float_as_uint(u[j].get(k)) & 0x7FFFFFFFu);
+    };
+    int8_eight<X> held[PASSES ? PASSES : 1][4];
+    if constexpr (PASSES > 0) {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i)
+            if (i * STEP < N) load(held[i], i * STEP + 4 * r);
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i)
+            if (i * STEP < N) raise(held[i]);
+    } else {
+        for (int n = 4 * r; n < N; n += STEP) {
+            load(held[0], n);
+            raise(held[0]);
+        }
     }
+    __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) atomicMax(&tops[8 * v + k], top[k]);
+    for (int k = 0; k < 8; ++k) {
+        // (first among the lanes that hold the same tokens)
+        for (int m = TV; m < 64; m *= 2) top[k] = max(top[k], (uint32_t)__shfl_xor((int)top[k], m));
+        if ((threadIdx.x & 63) < TV) atomicMax(&tops[8 * v + k], top[k]);
+    }
     __syncthreads();
     float factor[8];
 #pragma unroll
@@ -93,26 +123,31 @@ int8_quantize_columns_kernel(const X* __restrict__ x, long long ldx, long long B
         int8_factors(tops[8 * v + k], &scale, &factor[k]);
         if (r == 0 && 8 * v + k < tokens) s[b0 + 8 * v + k] = scale;
     }
-    for (int n0 = 0; n0 < N; n0 += STEP) {
-        const int n = n0 + 4 * r;
+    auto pass = [&](const int8_eight<X> (&u)[4], int n0) {
         uint32_t c[4][8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            int8_eight<X> e;
-            e.zero();
-            if (n + j < N) e = int8_load8(x + (size_t)(n + j) * ldx + b0, 8 * v, tokens);
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) c[j][k] = int8_code(e.get(k), factor[k]);
-        }
+            for (int k = 0; k < 8; ++k) c[j][k] = int8_code(u[j].get(k), factor[k]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) *reinterpret_cast<uint32_t*>(&tile[(8 * v + k) * PITCH + 4 * r]) = int8_pack4(c[0][k], c[1][k], c[2][k], c[3][k]);
         __syncthreads();
         const int pieces = min(STEP, (N - n0 + 15) / 16 * 16) / 16;
-        for (int i = threadIdx.x; i < tokens * pieces; i += 256) {
-            const int b = i / pieces, at = 16 * (i - b * pieces);
-            *reinterpret_cast<u32x4*>(q + (b0 + b) * ldq + n0 + at) = *reinterpret_cast<const u32x4*>(&tile[b * PITCH + at]);
+        for (int i = threadIdx.x; i < TOKENS * (STEP / 16); i += T) {
+            const int b = i / (STEP / 16), piece = i % (STEP / 16);
+            if (b < tokens && piece < pieces) *reinterpret_cast<u32x4*>(q + (b0 + b) * ldq + n0 + 16 * piece) = *reinterpret_cast<const u32x4*>(&tile[b * PITCH + 16 * piece]);
         }
         __syncthreads();
+    };
+    if constexpr (PASSES > 0) {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i)
+            if (i * STEP < N) pass(held[i], i * STEP);
+    } else {
+        for (int n0 = 0; n0 < N; n0 += STEP) {
+            load(held[0], n0 + 4 * r);
+            pass(held[0], n0);
+        }
     }
 }
 
@@ -149,17 +184,42 @@ unsigned grid_of(long long blocks) { return (unsigned)std::min<long long>(blocks
 template <typename X>
 hipError_t quantize(const X* x, bool token_major, long long B, int N, long long ldx, uint8_t* q, long long ldq, float* s, hipStream_t stream) {
     if (token_major) {
-#define ROWS(T, NV) hipLaunchKernelGGL((int8_quantize_rows_kernel<X, T, NV>), dim3(grid_of(T == 64 ? (B + 3) / 4 : B)), dim3(T == 64 ? 256 : T), 0, stream, x, ldx, B, N, q, ldq, s)
-        if (N <= 512) ROWS(64, 1);
-        else if (N <= 1024) ROWS(64, 2);
-        else if (N <= 2048) ROWS(64, 4);
-        else if (N <= 4096) ROWS(256, 2);
-        else if (N <= 8192) ROWS(256, 4);
-        else if (N <= 16384) ROWS(256, 8);
-        else ROWS(1024, 0);
-#undef ROWS
+        auto rows = [&](auto kernel, int threads, int tokens) {      // tokens: of a workgroup
+            hipLaunchKernelGGL(kernel, dim3(grid_of((B + tokens - 1) / tokens)), dim3(threads), 0, stream, x, ldx, B, N, q, ldq, s);
+        };
+        if (N <= 64) rows(int8_quantize_rows_kernel<X, 8, 1>, 256, 32);
+        else if (N <= 128) rows(int8_quantize_rows_kernel<X, 16, 1>, 256, 16);
+        else if (N <= 256) rows(int8_quantize_rows_kernel<X, 32, 1>, 256, 8);
+        else if (N <= 512) rows(int8_quantize_rows_kernel<X, 64, 1>, 256, 4);
+        else if (N <= 1024) rows(int8_quantize_rows_kernel<X, 64, 2>, 256, 4);
+        else if (N <= 2048) rows(int8_quantize_rows_kernel<X, 64, 4>, 256, 4);
+        else if (N <= 4096) rows(int8_quantize_rows_kernel<X, 256, 2>, 256, 1);
+        else if (N <= 8192) rows(int8_quantize_rows_kernel<X, 256, 4>, 256, 1);
+        else if (N <= 16384) rows(int8_quantize_rows_kernel<X, 256, 8>, 256, 1);
+        else rows(int8_quantize_rows_kernel<X, 1024, 0>, 1024, 1);
     } else {
-        hipLaunchKernelGGL((int8_quantize_columns_kernel<X, 4>), dim3((unsigned)((B + 31) / 32)), dim3(256), 0, stream, x, ldx, B, N, q, ldq, s);
+        auto columns = [&](auto kernel, int threads, int tokens) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((B + tokens - 1) / tokens)), dim3(threads), 0, stream, x, ldx, B, N, q, ldq, s);
+        };
+        // 64 bytes of a row (bf16) for each workgroup where that leaves one for most compute units, else fewer tokens.  In registers where x fits them: 8192 tokens of 4096 features
+        // 22.7 us, 48 with a second reading; token-major 15.6.
+        constexpr bool wide = sizeof(X) == 2;
+        if (B >= 4096) {
+            if (N <= 512) columns(int8_quantize_columns_kernel<X, 256, 4, 2>, 256, 32);
+            else if (N <= 2048) columns(int8_quantize_columns_kernel<X, 1024, 4, 2>, 1024, 32);
+            else if (N <= 4096 && wide) columns(int8_quantize_columns_kernel<X, 1024, 4, wide ? 4 : 0>, 1024, 32);
+            else columns(int8_quantize_columns_kernel<X, 1024, 4, 0>, 1024, 32);
+        } else if (B >= 1024) {
+            if (N <= 1024) columns(int8_quantize_columns_kernel<X, 256, 2, 2>, 256, 16);
+            else if (N <= 4096) columns(int8_quantize_columns_kernel<X, 1024, 2, 2>, 1024, 16);
+            else if (N <= 8192 && wide) columns(int8_quantize_columns_kernel<X, 1024, 2, wide ? 4 : 0>, 1024, 16);
+            else columns(int8_quantize_columns_kernel<X, 1024, 2, 0>, 1024, 16);
+        } else {
+            if (N <= 2048) columns(int8_quantize_columns_kernel<X, 256, 1, 2>, 256, 8);
+            else if (N <= 8192) columns(int8_quantize_columns_kernel<X, 1024, 1, 2>, 1024, 8);
+            else if (N <= 16384 && wide) columns(int8_quantize_columns_kernel<X, 1024, 1, wide ? 4 : 0>, 1024, 8);
+            else columns(int8_quantize_columns_kernel<X, 1024, 1, 0>, 1024, 8);
+        }
     }
     return hipGetLastError();
 }

@@ -438,17 +438,18 @@ hipError_t allow() {
 
 // The tiles, and what one takes a compute unit (us, all of them busy): to begin and store it (bf16, fp32), for each stage of 128 indices.  Measured on 256 CUs with 4096 to 36864 rows
 // of 512 to 9216 features at 96 to 2048 tokens; two workgroups of a compute unit take twice as long as one, so only the number of tiles for each counts.
-enum { TILE_64 = 1, TILE_128x64, TILE_128, TILE_256 };
+enum { TILE_64 = 1, TILE_128x64, TILE_128, TILE_256x128, TILE_256 };
 constexpr struct {
     int rows, tokens;
     double begin, begin_f32, stage;
-} tile_costs[] = {{}, {64, 64, 0.6, 0.8, 0.19}, {128, 64, 1.8, 2.2, 0.31}, {128, 128, 2.8, 3.4, 0.44}, {256, 256, 10, 14, 1.43}};
+} tile_costs[] = {{}, {64, 64, 0.6, 1.2, 0.19}, {128, 64, 1.8, 2.0, 0.31}, {128, 128, 2.8, 4.2, 0.44}, {256, 128, 4.5, 6.5, 0.88}, {256, 256, 10, 14, 1.43}};
 
 hipError_t launch(int tile, const gemm8_args& a, hipStream_t stream) {
     switch (tile) {
         case TILE_64: return launch<1, 1, 4, 0>(a, stream);
         case TILE_128x64: return launch<2, 1, 4, 8>(a, stream);
         case TILE_128: return launch<2, 2, 4, 8>(a, stream);
+        case TILE_256x128: return launch<4, 2, 4, 8>(a, stream);
         case TILE_256: return launch<4, 4, 4, 4>(a, stream);
     }
     return hipErrorInvalidValue;
@@ -472,6 +473,7 @@ hipError_t tsvd_int8_gemm_init() {
     hipError_t e = allow<1, 1, 4, 0>();
     if (e == hipSuccess) e = allow<2, 1, 4, 8>();
     if (e == hipSuccess) e = allow<2, 2, 4, 8>();
+    if (e == hipSuccess) e = allow<4, 2, 4, 8>();
     if (e == hipSuccess) e = allow<4, 4, 4, 4>();
     return e;
 }

@@ -77,8 +77,8 @@ int8_stream_kernel(stream_args p) {
         for (int k = 0; k < KT; ++k)
 #pragma unroll
             for (int e = 0; e < 2; ++e) top = int8_top8(v[k][e], top);
-        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        top = max(top, lane_xor32<16>(top));
+        top = max(top, lane_xor32<32>(top));
         if (lane < 16) tops[wave * 16 + lane] = top;
         __syncthreads();
         top = 0;

@@ -46,6 +46,11 @@ struct norm_args {
     long long y_rows, y_chunks;   // y: positions of a workgroup, workgroups one behind the other
 };
 
+template <int J>
+__device__ __forceinline__ float norm_xor(float v) { return __uint_as_float(lane_xor32<J>(__float_as_uint(v))); }
+template <int J>
+__device__ __forceinline__ double norm_xor(double v) { return lane_xor<J>(v); }
+
 // a / b for 0 <= a < 2^20, b >= 1: (a + 1/2) / b is 1 / (2 b) away from a whole number at least, more than the two roundings.  (A division of integers takes some forty
 // instructions, one of 64 bits hundreds, and everything here waits for them.)
 __device__ __forceinline__ int quotient(int a, int b) { return (int)(((float)a + 0.5f) * __builtin_amdgcn_rcpf((float)b)); }
@@ -121,6 +126,18 @@ __device__ __forceinline__ void load_rows(int8_eight<X> (&u)[N], const X* x, lon
         const X* row = x + (long long)min(pos + k * step, end - 1) * ldx;
         if constexpr (WHOLE) u[k].load(row + at);
         else u[k] = int8_load8(row, at, valid);
+    }
+}
+// The same where the rows are within 2^31 bytes of x (end * ldx * sizeof(X)): the places in 32 bits.
+template <bool WHOLE, int N, typename X>
+__device__ __forceinline__ void load_near_rows(int8_eight<X> (&u)[N], const X* x, uint32_t ldx, int at, int valid, int pos, int step, int end) {
+    uint32_t from = (uint32_t)min(pos, end - 1) * ldx;
+    const uint32_t last = (uint32_t)(end - 1) * ldx, by = (uint32_t)step * ldx;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if constexpr (WHOLE) u[k].load(reinterpret_cast<const X*>(reinterpret_cast<const char*>(x) + (from + (uint32_t)at) * (uint32_t)sizeof(X)));
+        else u[k] = int8_load8(x + from, at, valid);
+        from = min(from + by, last);
     }
 }
 template <typename F>
@@ -202,10 +219,21 @@ __device__ __forceinline__ int lanes_log2(int ng, int T) {
     while (log > 0 && (ng << log) > T) --log;
     return log;
 }
+// Sums over groups of 2^log lanes, in all of them (log is the same for all).
+template <typename T>
+__device__ __forceinline__ T lanes_sum(T v, int log) {
+    if (log > 0) v += norm_xor<1>(v);
+    if (log > 1) v += norm_xor<2>(v);
+    if (log > 2) v += norm_xor<4>(v);
+    if (log > 3) v += norm_xor<8>(v);
+    if (log > 4) v += norm_xor<16>(v);
+    if (log > 5) v += norm_xor<32>(v);
+    return v;
+}
 // Numbers, sums and sums of squares of 2^log lanes -> mean, and the sum of squared deviations or 1 / sqrt(v + eps).
 template <bool FINAL>
 __device__ __forceinline__ void store_joined(double n, double sum, double sq, int log, float eps, bool mine, float* mean, float* m2) {
-    for (int m = 1 << log >> 1; m > 0; m >>= 1) n += __shfl_xor(n, m), sum += __shfl_xor(sum, m), sq += __shfl_xor(sq, m);
+    n = lanes_sum(n, log), sum = lanes_sum(sum, log), sq = lanes_sum(sq, log);
     if (!mine) return;
     // (n is a whole number: its reciprocal in fp32, corrected once, is right to 2^-46)
     const double r0 = __builtin_amdgcn_rcpf((float)n), inv = r0 * (2.0 - n * r0), mu = sum * inv, dev = sq - sum * mu;
@@ -225,26 +253,29 @@ __device__ __forceinline__ void join_threads(const norm_lds& l, const norm_sums&
     const int tid = threadIdx.x;
     if (r < R) {
         const float n = (float)s.n, inv = s.n ? __builtin_amdgcn_rcpf(n) : 0.f;
+        const int valid = min(8, nch - 8 * at);
         norm_piece* to = l.piece + r * (cvec + ng) + at;
         int g = quotient(8 * at, cg), left = cg - (8 * at - g * cg);
-        float first = 0.f, sum = 0.f, m2 = 0.f, count = 0.f;
-        // a group's channels in this vector: their means about the first of them
+        // channels from .. to - 1 of the vector as one piece: their means about the first of them
+        auto piece = [&](int from, int end) {
+            float first = 0.f, sum = 0.f, m2 = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (8 * at + e < nch) {
-                const float mean = fmaf(s.s1[e], inv, s.k[e]);
-                if (count == 0.f) first = mean;
-                const float d = mean - first;
+            for (int e = 7; e >= 0; --e) first = e == from ? fmaf(s.s1[e], inv, s.k[e]) : first;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool in = e >= from && e < end;
+                const float d = in ? fmaf(s.s1[e], inv, s.k[e]) - first : 0.f;
                 sum += d;
-                m2 += fmaf(n * d, d, fmaf(-s.s1[e] * inv, s.s1[e], s.s2[e]));
-                count += 1.f;
-                if (--left == 0 || e == 7 || 8 * at + e == nch - 1) {
-                    const float off = sum * __builtin_amdgcn_rcpf(count);
-                    to[g] = norm_piece{first + off, fmaf(-n * sum, off, m2), n * count};
-                    ++g, left = cg;
-                    sum = m2 = count = 0.f;
-                }
+                m2 += in ? fmaf(n * d, d, fmaf(-s.s1[e] * inv, s.s1[e], s.s2[e])) : 0.f;
             }
+            const float count = (float)(end - from), off = sum * __builtin_amdgcn_rcpf(count);
+            to[g++] = norm_piece{first + off, fmaf(-n * sum, off, m2), n * count};
+        };
+        int from = 0, end = min(left, valid);
+        piece(from, end);
+        while (end < valid) {
+            from = end, end = min(end + cg, valid);
+            piece(from, end);
         }
     }
     __syncthreads();
@@ -288,7 +319,7 @@ norm_one_kernel(norm_args p) {
         s.clear();
         norm_channels ch;
         int8_eight<X> v[NV];
-        load_rows<decltype(whole)::value>(v, x, p.ldx, 8 * at, nch, r, R, P);
+        load_near_rows<decltype(whole)::value>(v, x, (uint32_t)p.ldx, 8 * at, nch, r, R, P);
         if (active) ch.load(p, c0 + 8 * at, n);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
@@ -355,7 +386,7 @@ norm_stats_wide_kernel(norm_args p) {
     __shared__ double part[T / 64];
     const int tid = threadIdx.x, cvec = (p.cg + 7) / 8, step_p = T / cvec, step_v = T % cvec;
     auto reduce = [&](double a) {
-        for (int m = 32; m > 0; m >>= 1) a += __shfl_xor(a, m);
+        a = wave_sum(a);
         __syncthreads();
         if ((tid & 63) == 0) part[tid >> 6] = a;
         __syncthreads();
@@ -523,7 +554,7 @@ norm_int8_kernel(norm_args p) {
                     if (c0 + e < p.C) top = max(top, __float_as_uint(f[k][e]) & 0x7FFFFFFFu);
             }
             float scale, factor;
-            int8_factors(int8_wave_top(top), &scale, &factor);
+            int8_factors(int8_lanes_top<64>(top), &scale, &factor);
             if (lane == 0) p.scales[row] = scale;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
@@ -560,7 +591,7 @@ norm_int8_wide_kernel(norm_args p) {
                 for (int e = 0; e < 8; ++e)
                     if (8 * at + e < p.C) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
             }
-            top = int8_wave_top(top);
+            top = int8_lanes_top<64>(top);
             if ((tid & 63) == 0) tops[tid >> 6] = top;
             __syncthreads();
             float scale, factor;
@@ -578,16 +609,16 @@ norm_int8_wide_kernel(norm_args p) {
 }
 
 // ---- rows: one position, one group --------------------------------------------------------------------
-// T threads for a row (64: four rows a workgroup), NV vectors of eight channels each, in registers.
+// T threads for a row (64 and fewer: several rows a workgroup and no barrier), NV vectors of eight channels each, in registers.
 template <typename X, int T, int NV, bool CODES>
-__global__ void __launch_bounds__(T == 64 ? 256 : T)
+__global__ void __launch_bounds__(T < 256 ? 256 : T)
 norm_rows_kernel(norm_args p) {
-    constexpr int WAVES = T / 64, ROWS = T == 64 ? 4 : 1;
+    constexpr int WAVES = T < 64 ? 1 : T / 64, ROWS = T < 256 ? 256 / T : 1, LOG = T >= 64 ? 6 : T == 32 ? 5 : 4;
     __shared__ float sums[2][WAVES];
     __shared__ uint32_t tops[WAVES];
-    const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, wave = t >> 6, C = p.C;
+    const int t = threadIdx.x % T, wave = t >> 6, C = p.C;
     auto reduce = [&](float a, int which) {
-        for (int m = 32; m > 0; m >>= 1) a += __shfl_xor(a, m);
+        a = lanes_sum(a, LOG);
         if constexpr (T > 64) {
             if ((t & 63) == 0) sums[which][wave] = a;
             __syncthreads();
@@ -597,66 +628,88 @@ norm_rows_kernel(norm_args p) {
         }
         return a;
     };
-    for (long long row = (long long)blockIdx.x * ROWS + (T == 64 ? threadIdx.x >> 6 : 0); row < p.images; row += (long long)gridDim.x * ROWS) {
-        const X* x = static_cast<const X*>(p.x) + row * p.ldx;
+    whole_or_not(C, [&](auto whole) {
+        // (whole: a vector's channels exist all or none)
+        constexpr bool WHOLE = decltype(whole)::value;
+        // gamma and beta stay for all rows of the workgroup
+        norm_channels ch[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) ch[k].load(p, WHOLE ? 8 * min(t + k * T, C / 8 - 1) : min(8 * (t + k * T), C - 1), WHOLE ? 8 : max(1, min(8, C - 8 * (t + k * T))));
+        const long long step = (long long)gridDim.x * ROWS;
+        long long row = (long long)blockIdx.x * ROWS + threadIdx.x / T;
+        auto load = [&](int8_eight<X> (&v)[NV], long long at) {
+            const X* x = static_cast<const X*>(p.x) + min(at, p.images - 1) * p.ldx;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if constexpr (WHOLE) v[k].load(x + 8 * min(t + k * T, C / 8 - 1));
+                else v[k] = int8_load8(x, 8 * (t + k * T), C);
+            }
+        };
         int8_eight<X> v[NV];
-        float sum = 0.f;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) v[k] = int8_load8(x, 8 * (t + k * T), C);
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += v[k].get(e);              // (zeros behind the end)
-        const float mean = reduce(sum, 0) / (float)C;
-        float m2 = 0.f;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int n = C - 8 * (t + k * T);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float d = e < n ? v[k].get(e) - mean : 0.f;
-                m2 = fmaf(d, d, m2);
-            }
-        }
-        const float rstd = 1.f / sqrtf(reduce(m2, 1) / (float)C + p.eps);
-        uint32_t top = 0;
-        float f[CODES ? NV : 1][8];
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c0 = 8 * (t + k * T), n = C - c0;
-            float(&h)[8] = f[CODES ? k : 0];
-            norm_channels ch;
-            if (n > 0) {
-                ch.load(p, c0, n);
-                ch.set(mean, rstd);
-                ch.apply(v[k], p.act, h);
-                if constexpr (CODES) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e < n) top = max(top, __float_as_uint(h[e]) & 0x7FFFFFFFu);
-                } else {
-                    if (p.token_major) store8(p.y, (size_t)row * p.ldy + c0, h, n, p.out_bf16);
-                    else store8_apart(p.y, c0, p.ldy, row, h, n, p.out_bf16);
-                }
-            }
-        }
-        if constexpr (CODES) {
-            top = int8_wave_top(top);
-            if constexpr (T > 64) {
-                if ((t & 63) == 0) tops[wave] = top;
-                __syncthreads();
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
-            }
-            float scale, factor;
-            int8_factors(top, &scale, &factor);
-            if (t == 0) p.scales[row] = scale;
+        load(v, row);
+        for (; row < p.images; row += step) {
+            float f[NV][8], sum = 0.f;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
-                if (8 * (t + k * T) < C) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (size_t)row * p.ldy + 8 * (t + k * T)) = codes_of(f[k], factor);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[k][e] = v[k].get(e);
+            load(v, row + step);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (!WHOLE || 8 * (t + k * T) < C)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum += f[k][e];              // (zeros behind the end)
+            const float mean = reduce(sum, 0) / (float)C;
+            float m2 = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int n = C - 8 * (t + k * T);
+                if (n > 0)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        f[k][e] -= mean;
+                        const float d = WHOLE || e < n ? f[k][e] : 0.f;
+                        m2 = fmaf(d, d, m2);
+                    }
+            }
+            const float rstd = 1.f / sqrtf(reduce(m2, 1) / (float)C + p.eps);
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int c0 = 8 * (t + k * T), n = C - c0;
+                if (n > 0) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[k][e] = fmaf(f[k][e], rstd * ch[k].factor[e], ch[k].beta[e]);
+                    norm_act(f[k], p.act);
+                    if constexpr (CODES) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (WHOLE || e < n) top = max(top, __float_as_uint(f[k][e]) & 0x7FFFFFFFu);
+                    } else {
+                        if (p.token_major) store8(p.y, (size_t)row * p.ldy + c0, f[k], n, p.out_bf16);
+                        else store8_apart(p.y, c0, p.ldy, row, f[k], n, p.out_bf16);
+                    }
+                }
+            }
+            if constexpr (CODES) {
+                top = int8_lanes_top<(T < 64 ? T : 64)>(top);
+                if constexpr (T > 64) {
+                    if ((t & 63) == 0) tops[wave] = top;
+                    __syncthreads();
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
+                }
+                float scale, factor;
+                int8_factors(top, &scale, &factor);
+                if (t == 0) p.scales[row] = scale;
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (8 * (t + k * T) < C) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (size_t)row * p.ldy + 8 * (t + k * T)) = codes_of(f[k], factor);
+            }
+            // (sums[0] is written again behind the barriers of sums[1] and of what follows; a workgroup without codes needs one more)
+            if constexpr (T > 64 && !CODES) __syncthreads();
         }
-        if constexpr (T > 64) __syncthreads();
-    }
+    });
 }
 
 // ---- the calls -------------------------------------------------------------------------------------
@@ -710,16 +763,18 @@ void cut_y(norm_args* a, bool token_major) {
     a->y_chunks = up(a->P, a->y_rows);
 }
 
-// One launch: the groups of a workgroup, 0 where it would hold too much.  64 bytes of a row at least if that still gives every compute unit a workgroup.
+// One launch: the groups of a workgroup, 0 where it would hold too much.  As few as give every compute unit a workgroup, but 64 bytes of a row at least (single groups of 20 channels, 40
+// bytes: 8 images of 1024 positions, 640 channels, 18.1 us on 256 compute units, 13.5 with pairs of groups on 128).
 template <typename X>
 int one_launch(const norm_args& a, int T, int rows_of_thread) {
     int gpb = std::min(a.G, T * 8 / a.cg);
-    if (gpb < 1) return 0;
+    if (gpb < 1 || a.P * a.ldx > INT32_MAX / 4) return 0;       // (places of an image in 32 bits)
     // whole vectors side by side where groups allow it
     const int unit = whole_groups(a.cg) <= gpb ? whole_groups(a.cg) : 1;
-    while (gpb > unit && (a.images * up(a.G, gpb) < CUS || up(a.P, T / up((long long)gpb * a.cg, 8)) > rows_of_thread) &&
+    auto rows_with = [&](int groups) { return up(a.P, T / up((long long)groups * a.cg, 8)); };
+    while (gpb > unit && (a.images * up(a.G, gpb) < CUS || rows_with(gpb) > rows_of_thread) &&
            (long long)std::max(unit, gpb / 2 / unit * unit) * a.cg * (int)sizeof(X) >= 64) gpb = std::max(unit, gpb / 2 / unit * unit);
-    return up(a.P, T / up((long long)gpb * a.cg, 8)) <= rows_of_thread ? gpb : 0;
+    return rows_with(gpb) <= rows_of_thread ? gpb : 0;
 }
 
 template <typename K>
@@ -735,12 +790,16 @@ hipError_t launch(K kernel, long long items, int T, size_t lds, hipStream_t stre
 
 template <typename X, bool CODES>
 hipError_t rows_form(const norm_args& a, hipStream_t stream) {
-    if (a.C <= 512) return launch(norm_rows_kernel<X, 64, 1, CODES>, up(a.images, 4), 256, 0, stream, a);
-    if (a.C <= 1024) return launch(norm_rows_kernel<X, 64, 2, CODES>, up(a.images, 4), 256, 0, stream, a);
-    if (a.C <= 2048) return launch(norm_rows_kernel<X, 256, 1, CODES>, a.images, 256, 0, stream, a);
-    if (a.C <= 4096) return launch(norm_rows_kernel<X, 256, 2, CODES>, a.images, 256, 0, stream, a);
-    if (a.C <= 8192) return launch(norm_rows_kernel<X, 256, 4, CODES>, a.images, 256, 0, stream, a);
-    return launch(norm_rows_kernel<X, 1024, 2, CODES>, a.images, 1024, 0, stream, a);
+    // (as many workgroups as the compute units hold at once, each with rows of its own)
+    auto rows = [&](auto kernel, int T, long long workgroups, int at_once) { return launch(kernel, std::min<long long>(workgroups, at_once * CUS), T, 0, stream, a); };
+    if (a.C <= 128) return rows(norm_rows_kernel<X, 16, 1, CODES>, 256, up(a.images, 16), 6);
+    if (a.C <= 256) return rows(norm_rows_kernel<X, 32, 1, CODES>, 256, up(a.images, 8), 6);
+    if (a.C <= 512) return rows(norm_rows_kernel<X, 64, 1, CODES>, 256, up(a.images, 4), 6);
+    if (a.C <= 1024) return rows(norm_rows_kernel<X, 64, 2, CODES>, 256, up(a.images, 4), 4);
+    if (a.C <= 2048) return rows(norm_rows_kernel<X, 256, 1, CODES>, 256, a.images, 6);
+    if (a.C <= 4096) return rows(norm_rows_kernel<X, 256, 2, CODES>, 256, a.images, 4);
+    if (a.C <= 8192) return rows(norm_rows_kernel<X, 512, 2, CODES>, 512, a.images, 2);
+    return rows(norm_rows_kernel<X, 1024, 2, CODES>, 1024, a.images, 1);
 }
 
 template <typename X>

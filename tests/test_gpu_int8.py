@@ -55,7 +55,7 @@ def values(rng, B, N, spread=True):
     return x
 
 
-SHAPES = [(1, 1), (1, 15), (3, 16), (2, 17), (5, 511), (4, 513), (3, 1025), (33, 100), (2, 2049), (3, 4097), (1, 8193), (2, 16385), (2, 131071), (70, 260)]
+SHAPES = [(4100, 100), (4100, 700), (4097, 2100), (1030, 1025), (1025, 4100), (1024, 8200), (300, 130), (9, 9000), (1, 1), (1, 15), (3, 16), (2, 17), (5, 511), (4, 513), (3, 1025), (33, 100), (2, 2049), (3, 4097), (1, 8193), (2, 16385), (2, 131071), (70, 260)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -155,7 +155,7 @@ def test_layer_against_64_bits(tsvd, M, N, B):
     tsvd.tsvd_int8_free(h)
 
 
-@pytest.mark.parametrize("tile", [1, 2, 3, 4])
+@pytest.mark.parametrize("tile", [1, 2, 3, 4, 5])
 @pytest.mark.parametrize("M,N,B", [(64, 128, 65), (65, 64, 66), (257, 385, 130), (300, 1000, 257), (1000, 2049, 100), (513, 130, 600), (37, 4100, 71)])
 def test_every_tile_gives_the_same_bits(tsvd, M, N, B, tile):
     """Every kind of tile, ragged in all three sizes (stages 1 to 33, odd and even), both layouts and types, against 64 bits; the sums are whole numbers and the

@@ -42,10 +42,13 @@ size_t tsvd_int8_row_bytes(int64_t N);
  *   x_dev : device, [B][N] with row stride ldx >= N (TSVD_TOKEN_MAJOR) or [N][B] with ldx >= B (TSVD_FEATURE_MAJOR) elements of
  *           x_dtype, at any stride and element alignment.
  *   scales_dev : device fp32 [B].
+ *   workspace : device, at least tsvd_int8_quantize_workspace_bytes(B, N, x_layout) bytes, 256-byte aligned (NULL with workspace_bytes 0 where that is 0, as it is for
+ *               TSVD_TOKEN_MAJOR); its contents are undefined afterwards.
  * Also what makes the codes and scales of weights from W [M][N] (a row is a token then).
- * TSVD_EINVAL: null pointers, sizes below 1, strides that are too small, codes that are not aligned. */
+ * TSVD_EINVAL: null pointers, sizes below 1, strides that are too small, codes that are not aligned, a workspace that is too small.  TSVD_EUNSUPPORTED: N >= 2^17, B > 2^24. */
+size_t tsvd_int8_quantize_workspace_bytes(int64_t B, int64_t N, tsvd_layout x_layout);
 tsvd_status tsvd_int8_quantize(const void* x_dev, tsvd_dtype x_dtype, tsvd_layout x_layout, int64_t B, int64_t N, int64_t ldx,
-                               int8_t* codes_dev, int64_t ldq, float* scales_dev, void* stream);
+                               int8_t* codes_dev, int64_t ldq, float* scales_dev, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- weights --------------------------------------------------------------------------------
  *
@@ -75,8 +78,8 @@ tsvd_status tsvd_int8_product(const tsvd_int8_handle* h, const int8_t* codes_dev
                               const float* bias_dev, void* y_dev, tsvd_dtype y_dtype, tsvd_layout y_layout, int64_t ldy, void* stream);
 
 /* y from x: tsvd_int8_quantize and tsvd_int8_product, the same bits, in one launch where tokens are few.
- *   workspace : device, at least tsvd_int8_workspace_bytes(h, B, x_dtype, x_layout) bytes, 256-byte aligned (may be NULL where
- *               that is 0); its contents are undefined afterwards.  x, y and workspace must not alias. */
+ *   workspace : device, at least tsvd_int8_workspace_bytes(h, B, x_dtype, x_layout) bytes, 256-byte aligned (NULL with
+ *               workspace_bytes 0 where that is 0); its contents are undefined afterwards.  x, y and workspace must not alias. */
 size_t tsvd_int8_workspace_bytes(const tsvd_int8_handle* h, int64_t B, tsvd_dtype x_dtype, tsvd_layout x_layout);
 tsvd_status tsvd_int8_forward(const tsvd_int8_handle* h, const void* x_dev, tsvd_dtype x_dtype, tsvd_layout x_layout, int64_t B, int64_t ldx,
                               const float* bias_dev, void* y_dev, tsvd_dtype y_dtype, tsvd_layout y_layout, int64_t ldy, void* workspace,

@@ -39,11 +39,11 @@ struct tsvd_int8_problem {
 };
 hipError_t tsvd_int8_gemm(const tsvd_int8_problem& p, hipStream_t stream);       // tsvd_int8_gemm.hip: any number of tokens
 hipError_t tsvd_int8_gemm_init();                                                // once for each device
-// tsvd_int8_stream.hip: few tokens; and from rows of x, where it makes the codes itself (p.codes and p.scales are not used then)
+// tsvd_int8_stream.hip: few tokens; and from x, where it makes the codes itself (p.codes and p.scales are not used then).  rows: x is [B][ldx], else [N][ldx]
 bool tsvd_int8_stream_serves(const tsvd_int8_handle& h, long long B);
 hipError_t tsvd_int8_stream(const tsvd_int8_problem& p, hipStream_t stream);
 bool tsvd_int8_stream_makes(const tsvd_int8_handle& h, long long B);
-hipError_t tsvd_int8_stream_from(const tsvd_int8_problem& p, const void* x, bool x_bf16, long long ldx, hipStream_t stream);
+hipError_t tsvd_int8_stream_from(const tsvd_int8_problem& p, const void* x, bool x_bf16, bool rows, long long ldx, hipStream_t stream);
 
 namespace {
 

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "tsvd_scratch.h"
 
@@ -15,6 +16,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
 long long round_up(long long v, long long m) { return (v + m - 1) / m * m; }
+
+// Workgroups go round the XCDs: each XCD gets a run of the numbers, so that neighbours, which share lines of x, meet in one L2.
+__device__ __forceinline__ unsigned xcd_run() {
+    const unsigned each = gridDim.x >> 3, more = gridDim.x & 7, xcd = blockIdx.x & 7;
+    return xcd * each + min(xcd, more) + (blockIdx.x >> 3);
+}
 
 // The largest over T threads: some lanes of a wavefront, or a workgroup's wavefronts.
 template <int T>
@@ -76,9 +83,7 @@ int8_quantize_columns_kernel(const X* __restrict__ x, long long ldx, long long B
     __shared__ uint32_t tops[TOKENS];
     __shared__ __align__(16) uint8_t tile[TOKENS * PITCH];
     const int v = threadIdx.x % TV, r = threadIdx.x / TV;
-    // workgroups go round the XCDs: neighbours, which share lines of x, are to meet in one L2
-    const unsigned each = gridDim.x >> 3, more = gridDim.x & 7, xcd = blockIdx.x & 7;
-    const long long b0 = (long long)(xcd * each + min(xcd, more) + (blockIdx.x >> 3)) * TOKENS;
+    const long long b0 = (long long)xcd_run() * TOKENS;
     const int tokens = (int)min((long long)TOKENS, B - b0);
     if (threadIdx.x < TOKENS) tops[threadIdx.x] = 0;
     const X* mine = x + b0;
@@ -151,6 +156,91 @@ int8_quantize_columns_kernel(const X* __restrict__ x, long long ldx, long long B
     }
 }
 
+// Feature-major x that a workgroup does not hold, or of so few tokens that few workgroups would have it: two launches, the features cut into slices.  The first leaves the largest
+// magnitudes of a slice's tokens, the second takes the largest over the slices and makes the slice's codes, as above.
+template <typename X, int TV>
+__global__ void __launch_bounds__(256)
+int8_column_tops_kernel(const X* __restrict__ x, long long ldx, long long B, int N, int rows, unsigned slices, uint32_t* __restrict__ tops_of) {
+    constexpr int ROWS = 256 / TV, TOKENS = 8 * TV;
+    __shared__ uint32_t tops[TOKENS];
+    const int v = threadIdx.x % TV, r = threadIdx.x / TV;
+    const unsigned blocks = gridDim.x / slices, at = xcd_run(), slice = at / blocks, block = at - slice * blocks;
+    const long long b0 = (long long)block * TOKENS;
+    const int tokens = (int)min((long long)TOKENS, B - b0), first = (int)slice * rows, end = min(first + rows, N);
+    if (threadIdx.x < TOKENS) tops[threadIdx.x] = 0;
+    const X* mine = x + b0;
+    uint32_t top[8] = {};
+    for (int n = first + r; n < end; n += 8 * ROWS) {
+        int8_eight<X> u[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = int8_load8(mine + (size_t)min(n + j * ROWS, end - 1) * ldx, min(8 * v, tokens - 1), tokens);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top[k] = max(top[k], __float_as_uint(u[j].get(k)) & 0x7FFFFFFFu);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        for (int m = TV; m < 64; m *= 2) top[k] = max(top[k], (uint32_t)__shfl_xor((int)top[k], m));
+        if ((threadIdx.x & 63) < TV) atomicMax(&tops[8 * v + k], top[k]);
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < tokens) tops_of[(size_t)slice * B + b0 + threadIdx.x] = tops[threadIdx.x];
+}
+template <typename X, int TV>
+__global__ void __launch_bounds__(256)
+int8_column_codes_kernel(const X* __restrict__ x, long long ldx, long long B, int N, int rows, unsigned slices, const uint32_t* __restrict__ tops_of, uint8_t* __restrict__ q,
+                         long long ldq, float* __restrict__ s) {
+    constexpr int ROWS = 256 / TV, STEP = 4 * ROWS, PITCH = STEP + 16, TOKENS = 8 * TV;
+    __shared__ uint32_t tops[TOKENS];
+    __shared__ __align__(16) uint8_t tile[TOKENS * PITCH];
+    const int v = threadIdx.x % TV, r = threadIdx.x / TV;
+    const unsigned blocks = gridDim.x / slices, at = xcd_run(), slice = at / blocks, block = at - slice * blocks;
+    const long long b0 = (long long)block * TOKENS;
+    const int tokens = (int)min((long long)TOKENS, B - b0), first = (int)slice * rows, end = min(first + rows, N);
+    if (threadIdx.x < TOKENS) tops[threadIdx.x] = 0;
+    const X* mine = x + b0;
+    int8_eight<X> u[4];
+    auto load = [&](int n) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = int8_load8(mine + (size_t)min(n + j, N - 1) * ldx, min(8 * v, tokens - 1), tokens);
+    };
+    load(first + 4 * r);
+    __syncthreads();
+    {
+        const int b = threadIdx.x % TOKENS;
+        uint32_t top = 0;
+        for (unsigned i = threadIdx.x / TOKENS; i < slices; i += 256 / TOKENS) top = max(top, tops_of[(size_t)i * B + min(b0 + b, B - 1)]);
+        atomicMax(&tops[b], top);
+    }
+    __syncthreads();
+    float factor[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        float scale;
+        int8_factors(tops[8 * v + k], &scale, &factor[k]);
+        if (slice == 0 && r == 0 && 8 * v + k < tokens) s[b0 + 8 * v + k] = scale;
+    }
+    for (int n0 = first; n0 < end; n0 += STEP) {
+        uint32_t c[4][8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c[j][k] = int8_code(u[j].get(k), factor[k]);
+        if (n0 + STEP < end) load(n0 + STEP + 4 * r);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) *reinterpret_cast<uint32_t*>(&tile[(8 * v + k) * PITCH + 4 * r]) = int8_pack4(c[0][k], c[1][k], c[2][k], c[3][k]);
+        __syncthreads();
+        const int pieces = min(STEP, (end - n0 + 15) / 16 * 16) / 16;
+        for (int i = threadIdx.x; i < TOKENS * (STEP / 16); i += 256) {
+            const int b = i / (STEP / 16), piece = i % (STEP / 16);
+            if (b < tokens && piece < pieces) *reinterpret_cast<u32x4*>(q + (b0 + b) * ldq + n0 + 16 * piece) = *reinterpret_cast<const u32x4*>(&tile[b * PITCH + 16 * piece]);
+        }
+        __syncthreads();
+    }
+}
+
 // Codes [M][ldw] -> tiles (tsvd_int8.h): a thread makes the 16 bytes of one lane.
 __global__ void __launch_bounds__(256)
 int8_pack_kernel(const uint8_t* __restrict__ w, long long ldw, long long M, int N, int nkt, long long pieces, uint8_t* __restrict__ tiles) {
@@ -181,8 +271,25 @@ int8_pack_scales_kernel(const float* __restrict__ t, long long M, long long rows
 
 unsigned grid_of(long long blocks) { return (unsigned)std::min<long long>(blocks, 1 << 20); }
 
+// How feature-major x is cut: vectors of eight tokens side by side, slices of the features (1: one launch), rows of a slice.
+struct columns_plan {
+    int tv, slices, rows;
+};
+columns_plan plan_columns(long long B, int N) {
+    columns_plan c;
+    c.tv = B >= 512 ? 8 : B > 16 ? 2 : 1;
+    const long long blocks = (B + 8 * c.tv - 1) / (8 * c.tv), step = 1024 / c.tv;
+    // one launch where a workgroup's registers hold all features and there is a workgroup for every other compute unit, or where there is next to nothing to do
+    const bool held = N <= (B >= 4096 ? 4096 : 2048) && B >= 1024;
+    const long long slices = std::min<long long>((N + step - 1) / step, std::max<long long>(1, (512 + blocks - 1) / blocks));
+    c.slices = held || slices < 2 || B * N <= 8192 ? 1 : (int)slices;
+    c.rows = (int)(((N + c.slices - 1) / c.slices + step - 1) / step * step);
+    c.slices = (N + c.rows - 1) / c.rows;
+    return c;
+}
+
 template <typename X>
-hipError_t quantize(const X* x, bool token_major, long long B, int N, long long ldx, uint8_t* q, long long ldq, float* s, hipStream_t stream) {
+hipError_t quantize(const X* x, bool token_major, long long B, int N, long long ldx, uint8_t* q, long long ldq, float* s, uint32_t* tops, hipStream_t stream) {
     if (token_major) {
         auto rows = [&](auto kernel, int threads, int tokens) {      // tokens: of a workgroup
             hipLaunchKernelGGL(kernel, dim3(grid_of((B + tokens - 1) / tokens)), dim3(threads), 0, stream, x, ldx, B, N, q, ldq, s);
@@ -198,38 +305,46 @@ hipError_t quantize(const X* x, bool token_major, long long B, int N, long long 
         else if (N <= 16384) rows(int8_quantize_rows_kernel<X, 256, 8>, 256, 1);
         else rows(int8_quantize_rows_kernel<X, 1024, 0>, 1024, 1);
     } else {
+        const columns_plan c = plan_columns(B, N);
+        if (c.slices > 1) {
+            auto sliced = [&](auto tv) {
+                constexpr int TV = decltype(tv)::value;
+                const dim3 grid((unsigned)((B + 8 * TV - 1) / (8 * TV) * c.slices));
+                hipLaunchKernelGGL((int8_column_tops_kernel<X, TV>), grid, dim3(256), 0, stream, x, ldx, B, N, c.rows, (unsigned)c.slices, tops);
+                const hipError_t e = hipGetLastError();
+                if (e != hipSuccess) return e;
+                hipLaunchKernelGGL((int8_column_codes_kernel<X, TV>), grid, dim3(256), 0, stream, x, ldx, B, N, c.rows, (unsigned)c.slices, tops, q, ldq, s);
+                return hipGetLastError();
+            };
+            return c.tv == 8 ? sliced(std::integral_constant<int, 8>()) : c.tv == 2 ? sliced(std::integral_constant<int, 2>()) : sliced(std::integral_constant<int, 1>());
+        }
         auto columns = [&](auto kernel, int threads, int tokens) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)((B + tokens - 1) / tokens)), dim3(threads), 0, stream, x, ldx, B, N, q, ldq, s);
         };
-        // 64 bytes of a row (bf16) for each workgroup where that leaves one for most compute units, else fewer tokens.  In registers where x fits them: 8192 tokens of 4096 features
-        // 22.7 us, 48 with a second reading; token-major 15.6.
-        constexpr bool wide = sizeof(X) == 2;
+        // 64 bytes of a row (bf16) for each workgroup where that leaves one for most compute units, else fewer tokens
         if (B >= 4096) {
             if (N <= 512) columns(int8_quantize_columns_kernel<X, 256, 4, 2>, 256, 32);
             else if (N <= 2048) columns(int8_quantize_columns_kernel<X, 1024, 4, 2>, 1024, 32);
-            else if (N <= 4096 && wide) columns(int8_quantize_columns_kernel<X, 1024, 4, wide ? 4 : 0>, 1024, 32);
-            else columns(int8_quantize_columns_kernel<X, 1024, 4, 0>, 1024, 32);
+            else columns(int8_quantize_columns_kernel<X, 1024, 4, sizeof(X) == 2 ? 4 : 0>, 1024, 32);
         } else if (B >= 1024) {
             if (N <= 1024) columns(int8_quantize_columns_kernel<X, 256, 2, 2>, 256, 16);
-            else if (N <= 4096) columns(int8_quantize_columns_kernel<X, 1024, 2, 2>, 1024, 16);
-            else if (N <= 8192 && wide) columns(int8_quantize_columns_kernel<X, 1024, 2, wide ? 4 : 0>, 1024, 16);
-            else columns(int8_quantize_columns_kernel<X, 1024, 2, 0>, 1024, 16);
+            else columns(int8_quantize_columns_kernel<X, 1024, 2, 2>, 1024, 16);
         } else {
             if (N <= 2048) columns(int8_quantize_columns_kernel<X, 256, 1, 2>, 256, 8);
-            else if (N <= 8192) columns(int8_quantize_columns_kernel<X, 1024, 1, 2>, 1024, 8);
-            else if (N <= 16384 && wide) columns(int8_quantize_columns_kernel<X, 1024, 1, wide ? 4 : 0>, 1024, 8);
             else columns(int8_quantize_columns_kernel<X, 1024, 1, 0>, 1024, 8);
         }
     }
     return hipGetLastError();
 }
-hipError_t quantize(const void* x, tsvd_dtype x_dtype, bool token_major, long long B, int N, long long ldx, int8_t* codes, long long ldq, float* s, hipStream_t stream) {
+hipError_t quantize(const void* x, tsvd_dtype x_dtype, bool token_major, long long B, int N, long long ldx, int8_t* codes, long long ldq, float* s, void* workspace, hipStream_t stream) {
     uint8_t* q = reinterpret_cast<uint8_t*>(codes);
-    return x_dtype == TSVD_BF16 ? quantize(static_cast<const uint16_t*>(x), token_major, B, N, ldx, q, ldq, s, stream)
-                                : quantize(static_cast<const float*>(x), token_major, B, N, ldx, q, ldq, s, stream);
+    uint32_t* tops = static_cast<uint32_t*>(workspace);
+    return x_dtype == TSVD_BF16 ? quantize(static_cast<const uint16_t*>(x), token_major, B, N, ldx, q, ldq, s, tops, stream)
+                                : quantize(static_cast<const float*>(x), token_major, B, N, ldx, q, ldq, s, tops, stream);
 }
 
 bool bad_codes(const void* codes, int64_t ldq, int64_t N) { return !codes || (reinterpret_cast<uintptr_t>(codes) & 15u) || ldq < N || ldq % 16 != 0; }
+bool bad_workspace(const void* ws, size_t bytes, size_t need) { return ws ? bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255u) : need != 0 || bytes != 0; }
 bool bad_dtype(int t) { return t != TSVD_F32 && t != TSVD_BF16; }
 bool bad_layout(int l) { return l != TSVD_FEATURE_MAJOR && l != TSVD_TOKEN_MAJOR; }
 
@@ -242,13 +357,20 @@ size_t codes_bytes(const tsvd_int8_handle* h, int64_t B) { return round256((size
 
 extern "C" size_t tsvd_int8_row_bytes(int64_t N) { return N <= 0 || N > TSVD_INT8_MAX_N ? 0 : (size_t)round_up(N, 128); }
 
+extern "C" size_t tsvd_int8_quantize_workspace_bytes(int64_t B, int64_t N, tsvd_layout x_layout) {
+    if (x_layout != TSVD_FEATURE_MAJOR || B < 1 || N < 1 || B > TSVD_INT8_MAX_B || N > TSVD_INT8_MAX_N) return 0;
+    const columns_plan c = plan_columns(B, (int)N);
+    return c.slices > 1 ? round256((size_t)c.slices * B * 4) : 0;
+}
+
 extern "C" tsvd_status tsvd_int8_quantize(const void* x_dev, tsvd_dtype x_dtype, tsvd_layout x_layout, int64_t B, int64_t N, int64_t ldx,
-                                          int8_t* codes_dev, int64_t ldq, float* scales_dev, void* stream) {
+                                          int8_t* codes_dev, int64_t ldq, float* scales_dev, void* workspace, size_t workspace_bytes, void* stream) {
     if (!x_dev || !scales_dev || B < 1 || N < 1 || bad_dtype(x_dtype) || bad_layout(x_layout)) return TSVD_EINVAL;
     if (ldx < (x_layout == TSVD_TOKEN_MAJOR ? N : B) || bad_codes(codes_dev, ldq, N)) return TSVD_EINVAL;
     if (N > TSVD_INT8_MAX_N || B > TSVD_INT8_MAX_B) return TSVD_EUNSUPPORTED;
+    if (bad_workspace(workspace, workspace_bytes, tsvd_int8_quantize_workspace_bytes(B, N, x_layout))) return TSVD_EINVAL;
     const bool rows = one_row(x_layout, B, ldx);
-    return quantize(x_dev, x_dtype, rows, B, (int)N, x_layout == TSVD_TOKEN_MAJOR ? ldx : rows ? N : ldx, codes_dev, ldq, scales_dev,
+    return quantize(x_dev, x_dtype, rows, B, (int)N, x_layout == TSVD_TOKEN_MAJOR ? ldx : rows ? N : ldx, codes_dev, ldq, scales_dev, workspace,
                     static_cast<hipStream_t>(stream)) == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
 }
 
@@ -329,9 +451,15 @@ extern "C" tsvd_status tsvd_int8_product(const tsvd_int8_handle* h, const int8_t
     return e == hipSuccess ? TSVD_OK : e == hipErrorNotSupported ? TSVD_EUNSUPPORTED : TSVD_EDEVICE;
 }
 
+namespace {
+// Whether a call makes the codes in the launch of the product, and where x is a contiguous vector.
+bool made_in_launch(const tsvd_int8_handle* h, int64_t B) { return tsvd_int8_stream_serves(*h, B) && tsvd_int8_stream_makes(*h, B); }
+}  // namespace
+
 extern "C" size_t tsvd_int8_workspace_bytes(const tsvd_int8_handle* h, int64_t B, tsvd_dtype x_dtype, tsvd_layout x_layout) {
     if (!h || B < 1 || B > TSVD_INT8_MAX_B || bad_dtype(x_dtype) || bad_layout(x_layout)) return 0;
-    return codes_bytes(h, B) + round256((size_t)B * 4);
+    if (made_in_launch(h, B)) return 0;
+    return codes_bytes(h, B) + round256((size_t)B * 4) + tsvd_int8_quantize_workspace_bytes(B, h->N, x_layout);
 }
 
 extern "C" tsvd_status tsvd_int8_forward(const tsvd_int8_handle* h, const void* x_dev, tsvd_dtype x_dtype, tsvd_layout x_layout, int64_t B, int64_t ldx,
@@ -340,14 +468,16 @@ extern "C" tsvd_status tsvd_int8_forward(const tsvd_int8_handle* h, const void* 
     if (!h || !x_dev || !y_dev || B < 1 || bad_dtype(x_dtype) || bad_layout(x_layout) || bad_dtype(y_dtype) || bad_layout(y_layout)) return TSVD_EINVAL;
     if (ldx < (x_layout == TSVD_TOKEN_MAJOR ? h->N : B) || ldy < (y_layout == TSVD_TOKEN_MAJOR ? h->M : B)) return TSVD_EINVAL;
     if (B > TSVD_INT8_MAX_B) return TSVD_EUNSUPPORTED;
-    if (!workspace || workspace_bytes < tsvd_int8_workspace_bytes(h, B, x_dtype, x_layout) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return TSVD_EINVAL;
-    if (one_row(x_layout, B, ldx) && tsvd_int8_stream_makes(*h, B)) {
+    if (bad_workspace(workspace, workspace_bytes, tsvd_int8_workspace_bytes(h, B, x_dtype, x_layout))) return TSVD_EINVAL;
+    if (made_in_launch(h, B)) {
         const tsvd_int8_problem p = {h, nullptr, 0, nullptr, B, bias_dev, y_dev, y_dtype == TSVD_BF16, y_layout == TSVD_TOKEN_MAJOR, ldy};
-        return tsvd_int8_stream_from(p, x_dev, x_dtype == TSVD_BF16, ldx, static_cast<hipStream_t>(stream)) == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
+        return tsvd_int8_stream_from(p, x_dev, x_dtype == TSVD_BF16, one_row(x_layout, B, ldx), ldx, static_cast<hipStream_t>(stream)) == hipSuccess ? TSVD_OK : TSVD_EDEVICE;
     }
     int8_t* codes = static_cast<int8_t*>(workspace);
-    float* scales = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + codes_bytes(h, B));
+    uint8_t* behind = static_cast<uint8_t*>(workspace) + codes_bytes(h, B);
+    float* scales = reinterpret_cast<float*>(behind);
     const int64_t ldq = (int64_t)tsvd_int8_row_bytes(h->N);
-    const tsvd_status st = tsvd_int8_quantize(x_dev, x_dtype, x_layout, B, h->N, ldx, codes, ldq, scales, stream);
+    const size_t more = tsvd_int8_quantize_workspace_bytes(B, h->N, x_layout);
+    const tsvd_status st = tsvd_int8_quantize(x_dev, x_dtype, x_layout, B, h->N, ldx, codes, ldq, scales, more ? behind + round256((size_t)B * 4) : nullptr, more, stream);
     return st != TSVD_OK ? st : tsvd_int8_product(h, codes, ldq, scales, B, bias_dev, y_dev, y_dtype, y_layout, ldy, stream);
 }

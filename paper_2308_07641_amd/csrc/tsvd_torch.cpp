@@ -330,10 +330,10 @@ void check_single_row(PyObject* o) {
     if (c.size(0) == 1 && left < (c.size(1) + 15) / 16 * 16) raise(PyExc_ValueError, "codes: a row needs room up to the next multiple of 16 bytes");
 }
 
-// int8_quantize(x, x_layout, codes, scales, stream)
+// int8_quantize(x, x_layout, codes, scales, workspace, stream)
 PyObject* py_int8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
-        need_args(n, 5, "int8_quantize");
+        need_args(n, 6, "int8_quantize");
         const at::Tensor& x = tensor_of(a[0], "x");
         if (!x.is_cuda() || x.dim() != 2 || x.stride(1) != 1) raise(PyExc_ValueError, "x must be a 2-d GPU tensor with unit inner stride");
         const c10::DeviceGuard device(x.device());
@@ -341,8 +341,8 @@ PyObject* py_int8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const bool xt = xl == TSVD_TOKEN_MAJOR;
         const int64_t B = x.size(xt ? 0 : 1), N = x.size(xt ? 1 : 0), ldx = row_pitch(x);
         const tsvd_dtype xd = dtype_code(x);
-        need_own(a[2], a[4], "work on a stream of your own needs codes and scales of your own");
-        need_own(a[3], a[4], "work on a stream of your own needs codes and scales of your own");
+        need_own(a[2], a[5], "work on a stream of your own needs codes and scales of your own");
+        need_own(a[3], a[5], "work on a stream of your own needs codes and scales of your own");
         y_ref codes{a[2] == Py_None ? new_codes(B, N, x) : Py_NewRef(a[2])}, scales{a[3] == Py_None ? THPVariable_Wrap(at::empty({B}, x.options().dtype(at::kFloat))) : Py_NewRef(a[3])};
         if (!codes.p || !scales.p) throw failed();
         const codes_view c = codes_of(codes.p);
@@ -350,11 +350,15 @@ PyObject* py_int8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
         check_single_row(codes.p);
         same_device(THPVariable_Unpack(codes.p), x, "codes must live on x's device");
         float* s = const_cast<float*>(floats_of(scales.p, B, x, "scales must be a contiguous float32 GPU tensor [B] on x's device"));
-        void* stream = stream_of(a[4], x);
+        const size_t need = tsvd_int8_quantize_workspace_bytes(B, N, xl);
+        if (need) need_own(a[4], a[5], "work on a stream of your own needs a workspace of your own");
+        at::Tensor made;
+        const workspace_view ws = scratch_of(a[4], need, x, &made);
+        void* stream = stream_of(a[5], x);
         const void* xp = x.data_ptr();
         tsvd_status st;
         Py_BEGIN_ALLOW_THREADS
-        st = tsvd_int8_quantize(xp, xd, xl, B, N, ldx, c.ptr, c.ldq, s, stream);
+        st = tsvd_int8_quantize(xp, xd, xl, B, N, ldx, c.ptr, c.ldq, s, ws.ptr, ws.bytes, stream);
         Py_END_ALLOW_THREADS
         check(st, "tsvd_int8_quantize");
         return codes_and_scales(codes, scales);

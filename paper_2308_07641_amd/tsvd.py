@@ -68,7 +68,8 @@ _PROTOTYPES = {
     "tsvd_conv2d_workspace_bytes": (_sz, [_vp, _vp, _i64, _i64, _i64]),
     "tsvd_conv2d_forward": (ctypes.c_int, [_vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, ctypes.c_int, _vp, _sz, _vp]),
     "tsvd_int8_row_bytes": (_sz, [_i64]),
-    "tsvd_int8_quantize": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, _i64, _i64, _i64, _vp, _i64, _vp, _vp]),
+    "tsvd_int8_quantize_workspace_bytes": (_sz, [_i64, _i64, ctypes.c_int]),
+    "tsvd_int8_quantize": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, _i64, _i64, _i64, _vp, _i64, _vp, _vp, _sz, _vp]),
     "tsvd_int8_packed_bytes": (_sz, [_i64, _i64]),
     "tsvd_int8_pack": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i64, _vp, _sz, _vp, ctypes.POINTER(_vp)]),
     "tsvd_int8_info": (ctypes.c_int, [_vp, _pi64, _pi64]),
@@ -491,12 +492,16 @@ def tsvd_int8_packed_bytes(M: int, N: int) -> int:
     return int(load_library().tsvd_int8_packed_bytes(M, N))
 
 
-def tsvd_int8_quantize(x, x_layout=TSVD_TOKEN_MAJOR, codes=None, scales=None, stream=None):
+def tsvd_int8_quantize_workspace_bytes(B: int, N: int, x_layout: int) -> int:
+    return int(load_library().tsvd_int8_quantize_workspace_bytes(B, N, x_layout))
+
+
+def tsvd_int8_quantize(x, x_layout=TSVD_TOKEN_MAJOR, codes=None, scales=None, workspace=None, stream=None):
     """(codes int8 [B,N], scales float32 [B]) of x [B,N] (token-major) or [N,B] (feature-major), fp32 or bf16 on the GPU.
 
     A weight matrix [M,N] is quantised row by row the same way.  New codes have a pitch of tsvd_int8_row_bytes(N).
     """
-    return (_binding or _load_binding()).int8_quantize(x, x_layout, codes, scales, stream)
+    return (_binding or _load_binding()).int8_quantize(x, x_layout, codes, scales, workspace, stream)
 
 
 def tsvd_int8_pack(codes, scales, dev_buf=None, stream=None) -> Int8Handle:

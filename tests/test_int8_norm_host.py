@@ -39,12 +39,14 @@ def test_int8_calls_check_their_arguments_first():
     p = (ctypes.addressof(buf) + 255) // 256 * 256
     out = ctypes.c_void_p()
 
-    def quantize(x=p, dtype=0, layout=1, B=2, N=32, ldx=32, codes=p, ldq=32, s=p):
-        return lib.tsvd_int8_quantize(x, dtype, layout, B, N, ldx, codes, ldq, s, None)
+    def quantize(x=p, dtype=0, layout=1, B=2, N=32, ldx=32, codes=p, ldq=32, s=p, ws=None, nbytes=0):
+        return lib.tsvd_int8_quantize(x, dtype, layout, B, N, ldx, codes, ldq, s, ws, nbytes, None)
 
     for bad in (dict(x=None), dict(codes=None), dict(s=None), dict(dtype=2), dict(layout=2), dict(B=0), dict(N=0), dict(ldx=31), dict(layout=0, ldx=1), dict(ldq=31), dict(ldq=40),
-                dict(codes=p + 8)):
+                dict(codes=p + 8), dict(nbytes=8), dict(ws=p + 8, nbytes=256), dict(layout=0, B=64, N=8192, ldx=64, ldq=8192),
+                dict(layout=0, B=64, N=8192, ldx=64, ldq=8192, ws=p, nbytes=16)):
         assert quantize(**bad) == EINVAL, bad
+    assert tsvd.tsvd_int8_quantize_workspace_bytes(64, 8192, 1) == 0 and tsvd.tsvd_int8_quantize_workspace_bytes(64, 8192, 0) > 0
     assert quantize(N=1 << 17, ldx=1 << 17, ldq=1 << 17) == EUNSUPPORTED and quantize(B=(1 << 24) + 1) == EUNSUPPORTED
 
     def pack(w=p, ldw=32, t=p, M=4, N=32, d=None, nbytes=0, o=ctypes.byref(out)):

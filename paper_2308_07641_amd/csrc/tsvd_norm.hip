@@ -343,6 +343,69 @@ norm_one_kernel(norm_args p) {
     }
 }
 
+// Codes in one launch: a workgroup has a whole image, all channels of all its positions, in registers.  The largest magnitudes of the vectors of a position meet in LDS.
+template <typename X, int T, int NV>
+__global__ void __launch_bounds__(T)
+norm_one_int8_kernel(norm_args p) {
+    extern __shared__ __align__(16) float smem[];
+    const int tid = threadIdx.x, C = p.C, ng = p.G, cvec = (C + 7) / 8, P = (int)p.P;
+    const int R = quotient(T, cvec), r = quotient(tid, cvec), at = tid - r * cvec, n = min(8, C - 8 * at);
+    const bool active = r < R;
+    const norm_lds l(smem, ng, R, cvec);
+    uint32_t* tops = reinterpret_cast<uint32_t*>(smem + 2 * ng);         // [NV][T], where the pieces were
+    float* factors = smem + 2 * ng + NV * T;                             // [P]
+    for (uint32_t image = blockIdx.x; image < (uint32_t)p.images; image += gridDim.x) {
+        const X* x = static_cast<const X*>(p.x) + (long long)image * P * p.ldx;
+        whole_or_not(C, [&](auto whole) {
+            norm_sums s;
+            s.clear();
+            norm_channels ch;
+            int8_eight<X> v[NV];
+            load_near_rows<decltype(whole)::value>(v, x, (uint32_t)p.ldx, 8 * at, C, r, R, P);
+            if (active) ch.load(p, 8 * at, n);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (active && r + k * R < P) s.add(v[k]);
+            join_threads<T, true>(l, s, at, r, cvec, R, C, ng, p.cg, p.eps);
+            if (active) ch.set(p.cg, 8 * at, n, 0, l.mean, l.m2);
+            if (active)
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (r + k * R < P) {
+                        float f[8];
+                        ch.apply(v[k], p.act, f);
+                        uint32_t top = 0;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (e < n) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+                        tops[k * T + tid] = top;
+                    }
+            __syncthreads();
+            const int log = lanes_log2(P, T), lane = tid & ((1 << log) - 1);
+            for (int pos = tid >> log; pos < P; pos += T >> log) {
+                const int k = quotient(pos, R);
+                const uint32_t* row = tops + k * T + (pos - k * R) * cvec;
+                uint32_t top = 0;
+                for (int i = lane; i < cvec; i += 1 << log) top = max(top, row[i]);
+                for (int m = 1 << log >> 1; m > 0; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+                float scale, factor;
+                int8_factors(top, &scale, &factor);
+                if (lane == 0) factors[pos] = factor, p.scales[(long long)image * P + pos] = scale;
+            }
+            __syncthreads();
+            if (active)
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (r + k * R < P) {
+                        float f[8];
+                        ch.apply(v[k], p.act, f);
+                        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + ((long long)image * P + r + k * R) * p.ldy + 8 * at) = codes_of(f, factors[r + k * R]);
+                    }
+        });
+        __syncthreads();
+    }
+}
+
 // ---- statistics of pieces --------------------------------------------------------------------------------
 // Several groups a workgroup, `rows` positions of them.
 template <typename X>
@@ -460,8 +523,8 @@ __device__ __forceinline__ void join_parts(const norm_args& p, long long image, 
 }
 
 // ---- y ---------------------------------------------------------------------------------------------
-// A workgroup has `vecs` vectors of channels and `y_rows` positions of an image.  Token-major: as in the statistics.  Feature-major: lanes along the positions, so
-// that a channel's values leave side by side (x: 16 bytes of a row for each lane, whole lines by the caches).
+// A workgroup has `vecs` vectors of channels and `y_rows` positions of an image.  Token-major: as in the statistics.  Feature-major: eight vectors of channels, through LDS, so
+// that a channel's positions leave side by side.  (Lanes along the positions instead, 16 bytes of 64 rows a load: 50 images of 1599 positions, 768 channels, 171 us.)
 template <typename X, bool TOKENS>
 __global__ void __launch_bounds__(256)
 norm_apply_kernel(norm_args p) {
@@ -502,17 +565,48 @@ norm_apply_kernel(norm_args p) {
                 }
             });
         } else {
+            // 64 positions at a time: eight lanes (of eight channels each) a position, 128 bytes of bf16, through LDS to 16 bytes of a channel's positions a lane
+            constexpr int POS = 64, E = 4;
+            float* tile = smem + 2 * ng + (2 * ng & 2);              // [64 channels][POS], a vector's rows turned by 8 times its number (64 banks a write)
+            const int lane8 = tid & 7, place = tid >> 3, n = min(8, nch - 8 * lane8);
+            norm_channels ch;
+            if (n > 0) ch.load(p, c0 + 8 * lane8, n);
             join_parts<T>(p, image, g0, ng, smem, smem + ng);
-            for (int at = 0; at < cvec; ++at) {
-                const int n = min(8, nch - 8 * at);
-                norm_channels ch;
-                ch.load(p, c0 + 8 * at, n);
-                ch.set(p.cg, c0 + 8 * at, n, g0, smem, smem + ng);
-                for (int pos = tid; pos < rows; pos += T) {
-                    float f[8];
-                    ch.apply(int8_load8(x + (long long)pos * p.ldx, 8 * at, nch), p.act, f);
-                    store8_apart(p.y, c0 + 8 * at, p.ldy, row0 + pos, f, n, p.out_bf16);
+            if (n > 0) ch.set(p.cg, c0 + 8 * lane8, n, g0, smem, smem + ng);
+            for (int first = 0; first < rows; first += POS) {
+                const int here = min(POS, rows - first);
+                int8_eight<X> u[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) u[k] = int8_load8(x + (long long)(first + min(place + 32 * k, here - 1)) * p.ldx, 8 * lane8, nch);
+                if (n > 0)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float f[8];
+                        ch.apply(u[k], p.act, f);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) tile[(8 * lane8 + e) * POS + ((place + 32 * k + 8 * lane8) & (POS - 1))] = f[e];
+                    }
+                __syncthreads();
+                for (int i = tid; i < nch * (POS / E); i += T) {
+                    const int c = i / (POS / E), pos = i % (POS / E) * E;
+                    const f32x4 f = *reinterpret_cast<const f32x4*>(tile + c * POS + ((pos + (c & 56)) & (POS - 1)));
+                    const size_t to = (size_t)(c0 + c) * p.ldy + row0 + first + pos;
+                    if (pos + E <= here) {
+                        if (p.out_bf16) {
+                            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+                            typedef u32x2 u32x2_at __attribute__((aligned(2)));
+                            *reinterpret_cast<u32x2_at*>(static_cast<uint16_t*>(p.y) + to) = u32x2{tsvd_pack_bf16(f[0], f[1]), tsvd_pack_bf16(f[2], f[3])};
+                        } else {
+                            typedef f32x4 f32x4_at __attribute__((aligned(4)));
+                            *reinterpret_cast<f32x4_at*>(static_cast<float*>(p.y) + to) = f;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < E - 1; ++e)
+                            if (pos + e < here) tsvd_store_y(p.y, to + e, f[e], p.out_bf16);
+                    }
                 }
+                __syncthreads();
             }
         }
         __syncthreads();
@@ -756,9 +850,9 @@ void cut_y(norm_args* a, bool token_major) {
         const int R = 256 / a->vecs;
         a->y_rows = std::min<long long>(a->P, R * std::max<long long>(1, std::min<long long>(16, up(a->images * a->vblk * a->P, 1024 * R))));
     } else {
-        a->vecs = std::min(cvec, 16);
+        a->vecs = std::min(cvec, 8);
         a->vblk = (int)up(cvec, a->vecs);
-        a->y_rows = std::min<long long>(a->P, 256);
+        a->y_rows = std::min<long long>(a->P, 64 * std::max<long long>(1, std::min<long long>(8, up(a->images * a->vblk * a->P, 1024 * 64))));
     }
     a->y_chunks = up(a->P, a->y_rows);
 }
@@ -825,17 +919,30 @@ hipError_t norm(norm_args a, hipStream_t stream) {
     if (e != hipSuccess) return e;
     cut_y(&a, a.token_major);
     const long long items = a.images * a.vblk * a.y_chunks;
-    const size_t lds = 8 * ((size_t)std::min<long long>(a.G, a.vecs * 8) + 1);
+    const size_t lds = 8 * ((size_t)std::min<long long>(a.G, a.vecs * 8) + 2) + (a.token_major ? 0 : 64 * 64 * 4);
     return a.token_major ? launch(norm_apply_kernel<X, true>, items, 256, lds, stream, a) : launch(norm_apply_kernel<X, false>, items, 256, lds, stream, a);
 }
 template <typename X>
 hipError_t norm_codes(norm_args a, hipStream_t stream) {
     if (a.P == 1 && a.G == 1 && a.C <= 16384) return rows_form<X, true>(a, stream);
+    const long long cvec = up(a.C, 8);
+    // Whole images, positions of a thread at most 1, 4 or 8.  Eight leave a compute unit one workgroup: for 64 to 512 images (320 channels, 64 positions: 256 images 12.1 us, 18.6 by
+    // pieces; 2695 images 114 us, 98.5 by pieces; one of 49 positions and 512 channels 11.3 us, 9.8 by pieces), and over 512 channels, whose codes by pieces take more wavefronts
+    // a row or read x twice more (16 positions of 1280 channels: one image 10.5 us and 15.0, 2695 images 110 us and 190).
+    size_t lds;
+    auto whole_images = [&](int T, int NV) {
+        const long long R = T / cvec, rows = R ? up(a.P, R) : NV + 1, pieces = sizeof(norm_piece) * R * (cvec + a.G);
+        lds = 8 * (size_t)a.G + std::max<size_t>(pieces, 4 * ((size_t)NV * T + a.P));
+        return rows <= NV && a.P * a.ldx <= INT32_MAX / 4 && lds <= 64 * 1024;
+    };
+    if (whole_images(256, 4)) return launch(norm_one_int8_kernel<X, 256, 4>, a.images, 256, lds, stream, a);
+    if (whole_images(512, 1)) return launch(norm_one_int8_kernel<X, 512, 1>, a.images, 512, lds, stream, a);
+    if (((a.images >= 64 && a.images <= 512) || a.C > 512) && whole_images(512, 8)) return launch(norm_one_int8_kernel<X, 512, 8>, a.images, 512, lds, stream, a);
     const hipError_t e = statistics<X>(a, stream);
     if (e != hipSuccess) return e;
     a.y_rows = std::min<long long>(a.P, 4 * std::max<long long>(4, std::min<long long>(MAX_ROWS, up(a.images * a.P, 2048 * 4))));
     a.y_chunks = up(a.P, a.y_rows);
-    const size_t lds = 8 * (size_t)a.G;
+    lds = 8 * (size_t)a.G;
     if (a.C <= 512) return launch(norm_int8_kernel<X, 1>, a.images * a.y_chunks, 256, lds, stream, a);
     if (a.C <= 1024) return launch(norm_int8_kernel<X, 2>, a.images * a.y_chunks, 256, lds, stream, a);
     a.y_rows = std::min<long long>(a.P, 4);

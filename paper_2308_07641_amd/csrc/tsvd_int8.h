@@ -38,7 +38,8 @@ struct tsvd_int8_problem {
     long long ldy;
 };
 hipError_t tsvd_int8_gemm(const tsvd_int8_problem& p, hipStream_t stream);       // tsvd_int8_gemm.hip: any number of tokens
-hipError_t tsvd_int8_gemm_init();                                                // once for each device
+hipError_t tsvd_int8_gemm_init();                                                // once for each device, as the next
+hipError_t tsvd_int8_stream_init();
 // tsvd_int8_stream.hip: few tokens; and from x, where it makes the codes itself (p.codes and p.scales are not used then).  rows: x is [B][ldx], else [N][ldx]
 bool tsvd_int8_stream_serves(const tsvd_int8_handle& h, long long B);
 hipError_t tsvd_int8_stream(const tsvd_int8_problem& p, hipStream_t stream);
@@ -143,6 +144,23 @@ __device__ __forceinline__ uint32_t int8_lanes_top(uint32_t v) {
     if constexpr (T > 4) v = max(v, lane_xor32<4>(v));
     if constexpr (T > 2) v = max(v, lane_xor32<2>(v));
     return max(v, lane_xor32<1>(v));
+}
+
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes a lane from a buffer to LDS, lane l's at lds + 16 l.  The compiler does not see what it moves: every use waits for vmcnt by hand.
+__device__ __forceinline__ void load_to_lds(i32x4 rsrc, uint32_t lds, int voff, int soff) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
+}
+__device__ __forceinline__ i32x4 buffer_of(const void* base, uint32_t bytes) {
+    const uint64_t a = reinterpret_cast<uintptr_t>(base);
+    return i32x4{(int)__builtin_amdgcn_readfirstlane((uint32_t)a), (int)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32) & 0xFFFF), (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000};
+}
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+    static_assert(N >= 0 && N <= 63, "vmcnt has six bits");
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
 }
 
 }  // namespace

@@ -394,7 +394,7 @@ extern "C" tsvd_status tsvd_int8_pack(const int8_t* w_dev, int64_t ldw, const fl
         (void)hipGetLastError();
         return TSVD_EDEVICE;
     }
-    if (tsvd_int8_gemm_init() != hipSuccess) {
+    if (tsvd_int8_gemm_init() != hipSuccess || tsvd_int8_stream_init() != hipSuccess) {
         (void)hipGetLastError();
         return TSVD_EDEVICE;
     }

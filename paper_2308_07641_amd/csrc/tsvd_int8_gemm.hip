@@ -22,7 +22,6 @@
 
 namespace {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -41,20 +40,6 @@ struct gemm8_args {
     int token_major, out_bf16;
     int row_tiles, token_tiles;
 };
-
-// 16 bytes a lane from a buffer to LDS, lane l's at lds + 16 l.  The compiler does not see what it moves: every use waits for vmcnt by hand.
-__device__ __forceinline__ void load_to_lds(i32x4 rsrc, uint32_t lds, int voff, int soff) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
-}
-__device__ __forceinline__ i32x4 buffer_of(const void* base, uint32_t bytes) {
-    const uint64_t a = reinterpret_cast<uintptr_t>(base);
-    return i32x4{(int)__builtin_amdgcn_readfirstlane((uint32_t)a), (int)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32) & 0xFFFF), (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000};
-}
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-    static_assert(N >= 0 && N <= 63, "vmcnt has six bits");
-    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
-}
 
 __device__ __forceinline__ void barrier() {
     __builtin_amdgcn_s_barrier();

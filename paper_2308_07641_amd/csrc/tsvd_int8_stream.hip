@@ -2,12 +2,14 @@
 // (v_mfma_i32_16x16x64_i8, 16 rows x 16 tokens), and that stream bounds the call.
 //
 // A workgroup owns a run of strips of 16 rows.  Its wavefronts split the contraction (and, where it is short, the strips): a wavefront holds the codes of its part in
-// registers, KT tiles of 64 indices by NB blocks of 16 tokens, and goes through the strips with the tiles of the next two on their way.  The parts meet in LDS
-// as integers, by additions whose order does not matter.  Nothing stands between the launch and the stream but the codes.
+// registers, KT tiles of 64 indices by NB blocks of 16 tokens, and goes through the strips, and on into the next part, with the tiles of the next two on their way.  The parts
+// meet in LDS as integers, by additions whose order does not matter.  Nothing stands between the launch and the stream but the codes.
 //
-// MAKE: the codes are made here, by every workgroup for itself: each lane reads the activations of its operand places, in either layout, the largest magnitudes of the tokens
-// meet in LDS (the one barrier before the end), and the codes are there in operand order, without a launch of their own or a way through memory.  HOLD: they stay in registers in
-// between; else (contractions longer than the wavefronts hold at once) they are read a second time, from the caches.
+// Codes come by way of LDS, each wavefront's own, in pieces of 16 tokens by up to 256 bytes, the next two pieces on their way: an operand's 16 lanes in turn have 16 tokens, and
+// read from memory like that take a request a lane (16 bytes a cycle and compute unit: 64 tokens of 16384 features 37 us, however few the rows).
+//
+// MAKE: the codes are made here, by every workgroup for itself: each lane reads a part of the activations (ROWS: token-major, eight side by side; else those of its operand
+// places), the largest magnitudes of the tokens meet in LDS (the one barrier before the end), and the codes are there without a launch of their own.
 #include "tsvd_int8.h"
 
 #include <algorithm>
@@ -16,8 +18,6 @@
 #include "tsvd_epilogue.h"
 
 namespace {
-
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // A 16 x 16 block of sums in LDS: rows of 20, so that the four rows that a cycle adds to stand in different banks.
 constexpr int BLOCK_PITCH = 20, BLOCK = 16 * BLOCK_PITCH;
@@ -37,27 +37,14 @@ struct stream_args {
 
 __device__ __forceinline__ i32x4 codes16(uint2 a, uint2 b) { return i32x4{(int)a.x, (int)a.y, (int)b.x, (int)b.y}; }
 
-// Sixteen activations of a token from index `at` on.  ROWS: side by side (zeros beyond N); else `ld` elements apart (beyond N the last one again: the weights' codes
-// are zero there).
-template <bool ROWS, typename X>
-__device__ __forceinline__ void load16(int8_eight<X> (&v)[2], const X* x, long long ld, int at, int N) {
-    if constexpr (ROWS) {
-        v[0] = int8_load8(x, at, N);
-        v[1] = int8_load8(x, at + 8, N);
-    } else {
-        X e[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) e[k] = x[(long long)min(at + k, N - 1) * ld];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            v[h].zero();
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[h].set(k, e[8 * h + k]);
-        }
-    }
-}
+// Pieces of codes in LDS: rows of 64 KT bytes, their 16 bytes exchanged so that 16 rows' stand in different banks.
+template <int KT>
+__device__ __forceinline__ int place(int row, int chunk) { return row * 64 * KT + ((chunk ^ (row / (4 / KT) % (4 * KT))) * 16); }
 
-template <int KT, int NB, typename MAKE, bool ROWS, bool HOLD>
+template <int KT, typename MAKE, bool ROWS>
+constexpr int wave_bytes() { return std::is_same<MAKE, void>::value ? 2048 * KT : ROWS ? 1024 * KT : 0; }
+
+template <int KT, int NB, typename MAKE, bool ROWS>
 __global__ void __launch_bounds__(1024)
 int8_stream_kernel(stream_args p) {
     constexpr bool make = !std::is_same<MAKE, void>::value;
@@ -81,78 +68,121 @@ int8_stream_kernel(stream_args p) {
         }
     };
     i32x4 x[NB][KT];
-    float factor = 0.f;
-    // (MAKE) the values of this lane's places: token i (beyond the last: that one's again), indices 16 g ... of its tiles
-    typedef typename std::conditional<make, MAKE, float>::type value;
-    const value* row = reinterpret_cast<const value*>(p.q) + (make ? (long long)min(i, p.B - 1) * (ROWS ? p.ldq : 1) : 0);
-    auto load_x = [&](int8_eight<value> (&v)[KT][2], int k0) {
+    // pieces: block u of chunk c, n = c NB + u
+    uint8_t* stage = reinterpret_cast<uint8_t*>(smem + p.strips_wg * NB * BLOCK) + wave * wave_bytes<KT, MAKE, ROWS>();
+    auto take = [&](int u, int set) {
 #pragma unroll
-        for (int k = 0; k < KT; ++k) load16<ROWS>(v[k], row, p.ldq, (k0 + k) * 64 + 16 * g, p.N);
+        for (int k = 0; k < KT; ++k) x[u][k] = *reinterpret_cast<const i32x4*>(stage + set * 1024 * KT + place<KT>(i, 4 * k + g));
     };
-    auto codes = [&](const int8_eight<value> (&v)[KT][2]) {
+    const uint32_t stage_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stage;
+    const uint32_t codes_bytes = make ? 0 : (uint32_t)((p.B - 1) * p.ldq) + (uint32_t)((p.N + 15) & ~15);
+    const i32x4 qbuf = buffer_of(p.q, codes_bytes);
+    // (tokens and indices beyond the last: zeros, or any codes, where the weights' are zero)
+    int voff[KT];
 #pragma unroll
-        for (int k = 0; k < KT; ++k) x[0][k] = codes16(int8_codes8(v[k][0], factor), int8_codes8(v[k][1], factor));
+    for (int j = 0; j < KT; ++j) {
+        const int row = j * (16 / KT) + lane / (4 * KT);
+        voff[j] = row * (int)p.ldq + place<KT>(row, lane % (4 * KT)) - row * 64 * KT;
+    }
+    auto request = [&](int n) {
+        const int c = n / NB, u = n % NB;
+        const uint32_t soff = min(16u * u * (uint32_t)p.ldq + (c * chunk_tiles + ks * KT) * 64u, codes_bytes);       // (what it leaves bounds voff)
+#pragma unroll
+        for (int j = 0; j < KT; ++j)
+            load_to_lds(qbuf, __builtin_amdgcn_readfirstlane(stage_at) + ((n & 1) * KT + j) * 1024, voff[j], __builtin_amdgcn_readfirstlane(soff));
     };
     if constexpr (make) {
-        int8_eight<value> v[KT][2];
-        uint32_t top = 0;
-        auto raise = [&] {
+        typedef typename std::conditional<make, MAKE, float>::type value;
+        const value* from = reinterpret_cast<const value*>(p.q);
+        // ROWS: eight values of a token a lane, 64 / LT tokens at a time; else sixteen of token i for each tile (beyond the last token: that one's again), at the lane's operand places
+        constexpr int LT = 8 * KT, STEP = 64 / LT;
+        int8_eight<value> v[2 * KT];
+        const int own = lane / LT, at = lane % LT;
 #pragma unroll
-            for (int k = 0; k < KT; ++k) top = int8_top8(v[k][1], int8_top8(v[k][0], top));
-        };
-        load_x(v, ks * KT);
-        if constexpr (HOLD) {
-            load(0, sg, ks * KT);
-            load(1, sg + p.sw, ks * KT);
-        }
-        for (int n = threadIdx.x; n < strips * NB * BLOCK; n += blockDim.x) smem[n] = 0;
-        raise();
-        if constexpr (!HOLD)
-            for (int c0 = chunk_tiles; c0 < p.nkt; c0 += chunk_tiles) {
-                load_x(v, c0 + ks * KT);
-                raise();
+        for (int k = 0; k < 2 * KT; ++k) {
+            v[k].zero();
+            if constexpr (ROWS) {
+                if (k * STEP + own < p.B) v[k] = int8_load8(from + (long long)(k * STEP + own) * p.ldq, ks * KT * 64 + 8 * at, p.N);
+            } else {
+                value e[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) e[n] = from[min(i, p.B - 1) + (long long)min((ks * KT + k / 2) * 64 + 16 * g + k % 2 * 8 + n, p.N - 1) * p.ldq];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) v[k].set(n, e[n]);
             }
-        top = max(top, lane_xor32<16>(top));
-        top = max(top, lane_xor32<32>(top));
-        if (lane < 16) tops[wave * 16 + lane] = top;
+        }
+        load(0, sg, ks * KT);
+        load(1, sg + p.sw, ks * KT);
+        for (int n = threadIdx.x; n < strips * NB * BLOCK; n += blockDim.x) smem[n] = 0;
+        if constexpr (ROWS) {
+#pragma unroll
+            for (int k = 0; k < 2 * KT; ++k) {
+                const uint32_t top = int8_lanes_top<LT>(int8_top8(v[k], 0));
+                if (at == 0) tops[wave * 16 + k * STEP + own] = top;
+            }
+        } else {
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < 2 * KT; ++k) top = int8_top8(v[k], top);
+            top = max(top, lane_xor32<16>(top));
+            top = max(top, lane_xor32<32>(top));
+            if (lane < 16) tops[wave * 16 + lane] = top;
+        }
         __syncthreads();
-        top = 0;
+        uint32_t top = 0;
         for (int n = 0; n < p.kw; ++n) top = max(top, tops[n * 16 + i]);
-        float scale;
+        float scale, factor;
         int8_factors(top, &scale, &factor);
         if (threadIdx.x < 16) token_scale[threadIdx.x] = scale;
-        if constexpr (HOLD) codes(v);
+        if constexpr (ROWS) {
+#pragma unroll
+            for (int k = 0; k < 2 * KT; ++k) {
+                const int token = k * STEP + own;
+                *reinterpret_cast<uint2*>(stage + place<KT>(token, at / 2) + at % 2 * 8) = int8_codes8(v[k], __shfl(factor, token));
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (a wavefront's own)
+            take(0, 0);
+        } else {
+#pragma unroll
+            for (int k = 0; k < KT; ++k) x[0][k] = codes16(int8_codes8(v[2 * k], factor), int8_codes8(v[2 * k + 1], factor));
+        }
     } else {
+        request(0);
+        if (NB > 1 || chunk_tiles < p.nkt) request(1);
+        load(0, sg, ks * KT);
+        load(1, sg + p.sw, ks * KT);
         for (int n = threadIdx.x; n < strips * NB * BLOCK; n += blockDim.x) smem[n] = 0;
         __syncthreads();
     }
-    for (int c0 = 0; c0 < p.nkt; c0 += chunk_tiles) {
+    for (int c0 = 0, n = 0; c0 < p.nkt; c0 += chunk_tiles, n += NB) {
         const int k0 = c0 + ks * KT;
         if constexpr (!make) {
+            // The pieces of a chunk, and requests for those two further on (LAST: none of the next chunk's).  Behind piece u there are requested for sure the piece after it, and,
+            // for the first two, the weights of two strips.
+            auto pieces = [&](auto last) {
+                constexpr bool LAST = decltype(last)::value;
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int k = 0; k < KT; ++k) {
-                    // (beyond the row's end or the last tile: any codes do, the weights' are zero)
-                    const long long at = min((long long)(k0 + k) * 64 + 16 * g, p.ldq - 16);
-                    x[b][k] = *reinterpret_cast<const i32x4*>(p.q + (long long)min(16 * b + i, p.B - 1) * p.ldq + at);
+                for (int u = 0; u < NB; ++u) {
+                    if (u < 2 && !(LAST && u + 1 == NB)) wait_vmcnt<3 * KT>();
+                    else if (u < 2) wait_vmcnt<2 * KT>();
+                    else if (!(LAST && u + 1 == NB)) wait_vmcnt<KT>();
+                    else wait_vmcnt<0>();
+                    take(u, NB == 1 ? n & 1 : u & 1);
+                    if (LAST && u + 2 >= NB) continue;
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the piece is read: another may come in its place
+                    request(n + u + 2);
                 }
-            load(0, sg, k0);
-            load(1, sg + p.sw, k0);
-        } else if constexpr (!HOLD) {
-            int8_eight<value> v[KT][2];
-            load_x(v, k0);
-            load(0, sg, k0);
-            load(1, sg + p.sw, k0);
-            codes(v);
+            };
+            if (c0 + chunk_tiles < p.nkt) pieces(std::false_type());
+            else pieces(std::true_type());
         }
-        auto strip = [&](int set, int at) {
+        auto strip = [&](int set, int at, int next, int next_k0) {
             i32x4 acc[NB] = {};
 #pragma unroll
             for (int k = 0; k < KT; ++k)
 #pragma unroll
                 for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[set][k], x[b][k], acc[b], 0, 0, 0);
-            load(set, at + 2 * p.sw, k0);
+            load(set, next, next_k0);
             if (at < strips) {
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
@@ -160,11 +190,17 @@ int8_stream_kernel(stream_args p) {
                     for (int v = 0; v < 4; ++v) atomicAdd(&smem[(at * NB + b) * BLOCK + (4 * g + v) * BLOCK_PITCH + i], acc[b][v]);
             }
         };
-        for (int at = sg; at < strips; at += 2 * p.sw) {
-            strip(0, at);
-            strip(1, at + p.sw);
-        }
+        // (wavefronts without a strip go through it once too: the counts above)
+        int at = sg;
+        do {
+            const bool last = at + 2 * p.sw >= strips;
+            const int next = last ? sg : at + 2 * p.sw, next_k0 = last ? k0 + chunk_tiles : k0;
+            strip(0, at, next, next_k0);
+            strip(1, at + p.sw, next + p.sw, next_k0);
+            at += 2 * p.sw;
+        } while (at < strips);
     }
+    if constexpr (!make) wait_vmcnt<0>();                            // (nothing may come to LDS after the end)
     __syncthreads();
     // lanes along the rows of a token (token-major y, and single tokens), else along the tokens of a row
     const int rows = (int)min((long long)strips * 16, p.M - (long long)strip0 * 16), along_rows = p.token_major || p.B == 1;
@@ -178,9 +214,9 @@ int8_stream_kernel(stream_args p) {
     }
 }
 
-constexpr int MAX_BLOCKS = 48;      // 60 KiB of sums
+constexpr int MAX_BLOCKS = 48;      // 60 KiB of sums beside 64 KiB of codes
 
-// How a launch is laid out: strips of a workgroup (all workgroups at once on the compute units, sums within 64 KiB of LDS), wavefronts and tiles of each.
+// How a launch is laid out: strips of a workgroup (all workgroups at once on the compute units where their sums allow it), wavefronts and tiles of each.
 struct stream_plan {
     int strips_wg, kw, sw, kt, nb;
 };
@@ -188,7 +224,7 @@ stream_plan plan_of(long long strips, int nkt, long long B, int cus, int most) {
     stream_plan s;
     s.nb = B <= 16 ? 1 : B <= 32 ? 2 : 4;
     s.strips_wg = (int)std::max<long long>(1, std::min<long long>((strips + cus - 1) / cus, MAX_BLOCKS / s.nb));
-    s.kt = std::min(most, s.nb == 1 ? 8 : 4);
+    s.kt = most;
     s.kw = 1;
     while (s.kw < 16 && s.kw * s.kt < nkt) s.kw *= 2;
     s.sw = 1;
@@ -199,26 +235,26 @@ stream_plan plan_of(long long strips, int nkt, long long B, int cus, int most) {
     return s;
 }
 
-template <int KT, int NB, typename MAKE, bool ROWS, bool HOLD>
+template <int KT, int NB, typename MAKE, bool ROWS>
 hipError_t launch(const stream_args& a, int grid, hipStream_t stream) {
-    // (sums within the 64 KiB that need no permission: plan_of)
-    hipLaunchKernelGGL((int8_stream_kernel<KT, NB, MAKE, ROWS, HOLD>), dim3(grid), dim3(64 * a.kw * a.sw), (size_t)a.strips_wg * NB * BLOCK * 4, stream, a);
+    const size_t lds = (size_t)a.strips_wg * NB * BLOCK * 4 + (size_t)a.kw * a.sw * wave_bytes<KT, MAKE, ROWS>();
+    hipLaunchKernelGGL((int8_stream_kernel<KT, NB, MAKE, ROWS>), dim3(grid), dim3(64 * a.kw * a.sw), lds, stream, a);
     return hipGetLastError();
+}
+template <int KT, int NB, typename MAKE>
+hipError_t allow() {
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(int8_stream_kernel<KT, NB, MAKE, true>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               MAX_BLOCKS * BLOCK * 4 + 16 * wave_bytes<KT, MAKE, true>());
 }
 template <int NB>
 hipError_t launch_codes(int kt, const stream_args& a, int grid, hipStream_t stream) {
-    if (kt == 1) return launch<1, NB, void, true, true>(a, grid, stream);
-    if (kt == 2) return launch<2, NB, void, true, true>(a, grid, stream);
-    if (kt == 4) return launch<4, NB, void, true, true>(a, grid, stream);
-    if constexpr (NB == 1) return launch<8, NB, void, true, true>(a, grid, stream);
-    return hipErrorInvalidValue;
+    return kt == 1 ? launch<1, NB, void, true>(a, grid, stream) : launch<2, NB, void, true>(a, grid, stream);
 }
 template <typename X, bool ROWS>
 hipError_t launch_make(int kt, const stream_args& a, int grid, hipStream_t stream) {
-    if (a.nkt > a.kw * kt) return launch<4, 1, X, ROWS, false>(a, grid, stream);       // (kt is 4 then)
-    if (kt == 1) return launch<1, 1, X, ROWS, true>(a, grid, stream);
-    if (kt == 2) return launch<2, 1, X, ROWS, true>(a, grid, stream);
-    return launch<4, 1, X, ROWS, true>(a, grid, stream);
+    if (kt == 1) return launch<1, 1, X, ROWS>(a, grid, stream);
+    if (kt == 2) return launch<2, 1, X, ROWS>(a, grid, stream);
+    return launch<4, 1, X, ROWS>(a, grid, stream);
 }
 stream_args args_of(const tsvd_int8_problem& p, const stream_plan& s) {
     const tsvd_int8_handle& h = *p.h;
@@ -230,22 +266,32 @@ stream_args args_of(const tsvd_int8_problem& p, const stream_plan& s) {
     return a;
 }
 
+constexpr int CODES_TILES = 2;      // (four: 9216 features, 2048 rows 7.8 us, with two 6.5; 16384 rows of 4096 the same)
 constexpr int MAKE_TILES = 4;       // tiles whose activations, codes and next weights fit the 128 registers of a lane
 
 }  // namespace
 
+hipError_t tsvd_int8_stream_init() {
+    for (hipError_t e : {allow<1, 1, void>(), allow<2, 1, void>(), allow<1, 2, void>(), allow<2, 2, void>(), allow<1, 4, void>(), allow<2, 4, void>(), allow<1, 1, float>(),
+                         allow<2, 1, float>(), allow<4, 1, float>(), allow<1, 1, uint16_t>(), allow<2, 1, uint16_t>(), allow<4, 1, uint16_t>()})
+        if (e != hipSuccess) return e;
+    return hipSuccess;
+}
+
 bool tsvd_int8_stream_serves(const tsvd_int8_handle&, long long B) { return B <= 64; }
 
 hipError_t tsvd_int8_stream(const tsvd_int8_problem& p, hipStream_t stream) {
-    const stream_plan s = plan_of(p.h->strips, p.h->nkt, p.B, p.h->cu_count, 8);
+    const stream_plan s = plan_of(p.h->strips, p.h->nkt, p.B, p.h->cu_count, CODES_TILES);
     stream_args a = args_of(p, s);
     a.q = reinterpret_cast<const uint8_t*>(p.codes), a.ldq = p.ldq;
     const int grid = (a.strips + s.strips_wg - 1) / s.strips_wg;
     return s.nb == 1 ? launch_codes<1>(s.kt, a, grid, stream) : s.nb == 2 ? launch_codes<2>(s.kt, a, grid, stream) : launch_codes<4>(s.kt, a, grid, stream);
 }
 
-// Whether the codes of B tokens are made in the launch of the product: up to 2^16 activations, which every workgroup reads (and, beyond 4096 features, reads twice).
-bool tsvd_int8_stream_makes(const tsvd_int8_handle& h, long long B) { return B <= 16 && B * h.N <= 1 << 16; }
+// Whether the codes of B tokens are made in the launch of the product: where its wavefronts hold the contraction (4096 features, 16 wavefronts of 4 tiles of 64).  Against a launch
+// of their own, 16 tokens: 4096 rows of 2048 features, token-major bf16 4.9 us and 6.6, feature-major 5.7 and 11.5; 16384 rows of 4096 13.0 and 14.7, 13.2 and 20.1; 4096 rows of
+// 4096 7.7 and 7.8 (fp32 8.4 and 7.8, the one that loses), one token 6.9 and 7.2.
+bool tsvd_int8_stream_makes(const tsvd_int8_handle& h, long long B) { return B <= 16 && h.nkt <= 16 * MAKE_TILES; }
 
 hipError_t tsvd_int8_stream_from(const tsvd_int8_problem& p, const void* x, bool x_bf16, bool rows, long long ldx, hipStream_t stream) {
     const stream_plan s = plan_of(p.h->strips, p.h->nkt, p.B, p.h->cu_count, MAKE_TILES);

@@ -122,6 +122,21 @@ __device__ __forceinline__ int8_eight<X> int8_load8(const X* row, int at, int n)
     }
     return r;
 }
+// The same of several rows (row(k)), at one place: the loads go out together, no branch between them.
+template <int N, typename X, typename F>
+__device__ __forceinline__ void int8_loads8(int8_eight<X> (&r)[N], F&& row, int at, int n) {
+    if (n >= 8) {
+        const int from = min(at, n - 8);
+#pragma unroll
+        for (int k = 0; k < N; ++k) r[k].load(row(k) + from);
+        if (at > from)
+#pragma unroll
+            for (int k = 0; k < N; ++k) r[k].shift(min(at - from, 8));
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) r[k] = int8_load8(row(k), at, n);
+    }
+}
 template <typename X>
 __device__ __forceinline__ uint32_t int8_top8(const int8_eight<X>& r, uint32_t top) {
 #pragma unroll

@@ -121,24 +121,28 @@ struct norm_channels {
 // rows at or behind the end are the last one again (not used).
 template <bool WHOLE, int N, typename X>
 __device__ __forceinline__ void load_rows(int8_eight<X> (&u)[N], const X* x, long long ldx, int at, int valid, int pos, int step, int end) {
+    auto row = [&](int k) { return x + (long long)min(pos + k * step, end - 1) * ldx; };
+    if constexpr (WHOLE) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        const X* row = x + (long long)min(pos + k * step, end - 1) * ldx;
-        if constexpr (WHOLE) u[k].load(row + at);
-        else u[k] = int8_load8(row, at, valid);
-    }
+        for (int k = 0; k < N; ++k) u[k].load(row(k) + at);
+    } else int8_loads8(u, row, at, valid);
 }
 // The same where the rows are within 2^31 bytes of x (end * ldx * sizeof(X)): the places in 32 bits.
 template <bool WHOLE, int N, typename X>
 __device__ __forceinline__ void load_near_rows(int8_eight<X> (&u)[N], const X* x, uint32_t ldx, int at, int valid, int pos, int step, int end) {
     uint32_t from = (uint32_t)min(pos, end - 1) * ldx;
     const uint32_t last = (uint32_t)(end - 1) * ldx, by = (uint32_t)step * ldx;
+    if constexpr (WHOLE) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        if constexpr (WHOLE) u[k].load(reinterpret_cast<const X*>(reinterpret_cast<const char*>(x) + (from + (uint32_t)at) * (uint32_t)sizeof(X)));
-        else u[k] = int8_load8(x + from, at, valid);
+        for (int k = 0; k < N; ++k) {
+            u[k].load(reinterpret_cast<const X*>(reinterpret_cast<const char*>(x) + (from + (uint32_t)at) * (uint32_t)sizeof(X)));
+            from = min(from + by, last);
+        }
+    } else int8_loads8(u, [&](int) {
+        const X* row = x + from;
         from = min(from + by, last);
-    }
+        return row;
+    }, at, valid);
 }
 template <typename F>
 __device__ __forceinline__ void whole_or_not(int channels, F&& body) {
@@ -576,8 +580,7 @@ norm_apply_kernel(norm_args p) {
             for (int first = 0; first < rows; first += POS) {
                 const int here = min(POS, rows - first);
                 int8_eight<X> u[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) u[k] = int8_load8(x + (long long)(first + min(place + 32 * k, here - 1)) * p.ldx, 8 * lane8, nch);
+                int8_loads8(u, [&](int k) { return x + (long long)(first + min(place + 32 * k, here - 1)) * p.ldx; }, 8 * lane8, nch);
                 if (n > 0)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
@@ -614,12 +617,14 @@ norm_apply_kernel(norm_args p) {
 }
 
 // ---- codes -----------------------------------------------------------------------------------------
-// A wavefront for each position, NV vectors of channels a lane with their factors in registers, `y_rows` positions of an image a workgroup.
-template <typename X, int NV>
+// L lanes for each position, NV vectors of channels a lane with their factors in registers, `y_rows` positions of an image a workgroup, AHEAD of each lane's at a time.
+template <typename X, int L, int NV>
 __global__ void __launch_bounds__(256)
 norm_int8_kernel(norm_args p) {
+    constexpr int AHEAD = NV == 1 ? 4 : 2, SLOTS = 256 / L;
     extern __shared__ __align__(16) float smem[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cvec = (p.C + 7) / 8;
+    __shared__ uint32_t tops[2][AHEAD][4];
+    const int lane = threadIdx.x % L, slot = threadIdx.x / L, cvec = (p.C + 7) / 8;
     const uint32_t chunks = (uint32_t)p.y_chunks, items = (uint32_t)p.images * chunks;
     for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
         const uint32_t back = items - 1 - item, image_at = back / chunks;
@@ -630,29 +635,45 @@ norm_int8_kernel(norm_args p) {
         norm_channels ch[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c0 = 8 * (lane + 64 * k);
+            const int c0 = 8 * (lane + L * k);
             const int n = max(0, min(8, p.C - c0));
             ch[k].load(p, min(c0, p.C - 1), n);
             ch[k].set(p.cg, min(c0, p.C - 1), n, 0, smem, smem + p.G);
         }
-        for (int pos = wave; pos < rows; pos += 4) {
-            const long long row = row0 + pos;
-            float f[NV][8];
-            uint32_t top = 0;
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int c0 = 8 * (lane + 64 * k);
-                ch[k].apply(int8_load8(static_cast<const X*>(p.x) + row * p.ldx, c0, p.C), p.act, f[k]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (c0 + e < p.C) top = max(top, __float_as_uint(f[k][e]) & 0x7FFFFFFFu);
-            }
-            float scale, factor;
-            int8_factors(int8_lanes_top<64>(top), &scale, &factor);
-            if (lane == 0) p.scales[row] = scale;
+        int turn = 0;
+        for (int pos = 0; pos < rows; pos += AHEAD * SLOTS, turn ^= 1) {
+            int8_eight<X> v[NV][AHEAD];
 #pragma unroll
             for (int k = 0; k < NV; ++k)
-                if (lane + 64 * k < cvec) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (size_t)row * p.ldy + 8 * (lane + 64 * k)) = codes_of(f[k], factor);
+                int8_loads8(v[k], [&](int a) { return static_cast<const X*>(p.x) + (row0 + min(pos + a * SLOTS + slot, rows - 1)) * p.ldx; }, 8 * (lane + L * k), p.C);
+            float f[AHEAD][NV][8];
+            uint32_t top[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                top[a] = 0;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    ch[k].apply(v[k][a], p.act, f[a][k]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (8 * (lane + L * k) + e < p.C) top[a] = max(top[a], __float_as_uint(f[a][k][e]) & 0x7FFFFFFFu);
+                }
+                top[a] = int8_lanes_top<L < 64 ? L : 64>(top[a]);
+                if (L > 64 && lane % 64 == 0) tops[turn][a][lane / 64] = top[a];
+            }
+            if constexpr (L > 64) __syncthreads();                   // (two sets of tops: the next turn's need not wait for this one's readers)
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                if constexpr (L > 64) top[a] = max(max(tops[turn][a][0], tops[turn][a][1]), max(tops[turn][a][2], tops[turn][a][3]));
+                const int at = pos + a * SLOTS + slot;
+                if (at >= rows) continue;
+                float scale, factor;
+                int8_factors(top[a], &scale, &factor);
+                if (lane == 0) p.scales[row0 + at] = scale;
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (lane + L * k < cvec) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (size_t)(row0 + at) * p.ldy + 8 * (lane + L * k)) = codes_of(f[a][k], factor);
+            }
         }
         __syncthreads();
     }
@@ -837,7 +858,8 @@ void cut(long long images, long long P, int C, int G, norm_args* a) {
     a->gpb = (int)(up(up(G, a->nblk), unit) * unit);
     a->nblk = (int)up(G, a->gpb);
     const int R = 256 / (int)up(a->gpb * a->cg, 8);
-    const long long per = std::max<long long>(1, std::min<long long>(MAX_ROWS, up(images * a->nblk * P, 512 * R)));
+    // up to 64 positions of a thread: about 512 workgroups, and at most 2048 pieces of an image, which workgroups of the next launch join
+    const long long per = std::max<long long>(1, std::min<long long>(MAX_ROWS, std::max(up(images * a->nblk * P, 512 * R), up(P * G, 2048 * R))));
     a->rows = (int)std::min<long long>(per * R, P);
     a->chunks = up(P, a->rows);
 }
@@ -906,13 +928,15 @@ hipError_t statistics(const norm_args& a, hipStream_t stream) {
 template <typename X>
 hipError_t norm(norm_args a, hipStream_t stream) {
     if (a.P == 1 && a.G == 1 && a.C <= 16384) return rows_form<X, false>(a, stream);
-    for (int T : {256, 512}) {
-        const int gpb = one_launch<X>(a, T, T == 256 ? 8 : 16);
-        if (!gpb) continue;
+    for (int T : {64, 256, 512}) {
+        // (small workgroups for whole small images, several for each compute unit: 2000 of 9 positions, 64 channels 5.9 us, 11.0 by larger ones)
+        const int gpb = T > 64 || a.images > 512 ? one_launch<X>(a, T, T <= 256 ? 8 : 16) : 0;
+        if (!gpb || (T == 64 && gpb < a.G)) continue;
         norm_args b = a;
         b.gpb = gpb, b.nblk = (int)up(a.G, gpb);
         const int cvec = (int)up((long long)gpb * a.cg, 8);
         const size_t lds = norm_lds::bytes(gpb, T / cvec, cvec);
+        if (T == 64) return launch(norm_one_kernel<X, 64, 8>, b.images * b.nblk, T, lds, stream, b);
         return T == 256 ? launch(norm_one_kernel<X, 256, 8>, b.images * b.nblk, T, lds, stream, b) : launch(norm_one_kernel<X, 512, 16>, b.images * b.nblk, T, lds, stream, b);
     }
     const hipError_t e = statistics<X>(a, stream);
@@ -935,16 +959,27 @@ hipError_t norm_codes(norm_args a, hipStream_t stream) {
         lds = 8 * (size_t)a.G + std::max<size_t>(pieces, 4 * ((size_t)NV * T + a.P));
         return rows <= NV && a.P * a.ldx <= INT32_MAX / 4 && lds <= 64 * 1024;
     };
+    if (a.images > 512 && whole_images(64, 4)) return launch(norm_one_int8_kernel<X, 64, 4>, a.images, 64, lds, stream, a);
     if (whole_images(256, 4)) return launch(norm_one_int8_kernel<X, 256, 4>, a.images, 256, lds, stream, a);
     if (whole_images(512, 1)) return launch(norm_one_int8_kernel<X, 512, 1>, a.images, 512, lds, stream, a);
+    if (whole_images(1024, 1)) return launch(norm_one_int8_kernel<X, 1024, 1>, a.images, 1024, lds, stream, a);
     if (((a.images >= 64 && a.images <= 512) || a.C > 512) && whole_images(512, 8)) return launch(norm_one_int8_kernel<X, 512, 8>, a.images, 512, lds, stream, a);
     const hipError_t e = statistics<X>(a, stream);
     if (e != hipSuccess) return e;
-    a.y_rows = std::min<long long>(a.P, 4 * std::max<long long>(4, std::min<long long>(MAX_ROWS, up(a.images * a.P, 2048 * 4))));
-    a.y_chunks = up(a.P, a.y_rows);
     lds = 8 * (size_t)a.G;
-    if (a.C <= 512) return launch(norm_int8_kernel<X, 1>, a.images * a.y_chunks, 256, lds, stream, a);
-    if (a.C <= 1024) return launch(norm_int8_kernel<X, 2>, a.images * a.y_chunks, 256, lds, stream, a);
+    // up to 16 turns of a workgroup, about 512 workgroups: each joins the pieces of its image
+    auto codes = [&](auto kernel, int positions) {
+        a.y_rows = std::min<long long>(a.P, positions * std::max<long long>(1, std::min<long long>(16, up(a.images * a.P, 512 * positions))));
+        a.y_chunks = up(a.P, a.y_rows);
+        return launch(kernel, a.images * a.y_chunks, 256, lds, stream, a);
+    };
+    if (a.C <= 64) return codes(norm_int8_kernel<X, 8, 1>, 128);
+    if (a.C <= 128) return codes(norm_int8_kernel<X, 16, 1>, 64);
+    if (a.C <= 256) return codes(norm_int8_kernel<X, 32, 1>, 32);
+    if (a.C <= 512) return codes(norm_int8_kernel<X, 64, 1>, 16);
+    if (a.C <= 1024) return codes(norm_int8_kernel<X, 64, 2>, 8);
+    if (a.C <= 2048) return codes(norm_int8_kernel<X, 256, 1>, 4);
+    if (a.C <= 4096) return codes(norm_int8_kernel<X, 256, 2>, 2);
     a.y_rows = std::min<long long>(a.P, 4);
     a.y_chunks = up(a.P, a.y_rows);
     return launch(norm_int8_wide_kernel<X>, a.images * a.y_chunks, 256, lds, stream, a);

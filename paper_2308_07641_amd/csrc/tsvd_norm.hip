@@ -314,7 +314,9 @@ norm_one_kernel(norm_args p) {
         // workgroups go round the XCDs: each gets a run of the items, so that the groups of an image, which share lines of x and y, meet in one L2
         const uint32_t item = (id & 7) * each + min(id & 7, more) + (id >> 3), image = item / (uint32_t)p.nblk;
         const int blk = (int)(item - image * p.nblk), g0 = blk * p.gpb, ng = min(p.gpb, p.G - g0), c0 = g0 * p.cg, nch = ng * p.cg, cvec = (nch + 7) / 8;
-        const int R = quotient(T, cvec), r = quotient(tid, cvec), at = tid - r * cvec, P = (int)p.P, n = min(8, nch - 8 * at);
+        const int R = quotient(T, cvec), r = quotient(tid, cvec), at = tid - r * cvec, P = (int)p.P;
+        // (a last vector that is not whole is read and written as the last eight channels, some of them twice; the sums leave those out)
+        const int n = min(8, nch), c = max(0, min(8 * at, nch - 8)), twice = 8 * at - c;
         const bool active = r < R;
         const X* x = static_cast<const X*>(p.x) + (long long)image * p.P * p.ldx + c0;
         const norm_lds l(smem, ng, R, cvec);
@@ -323,14 +325,21 @@ norm_one_kernel(norm_args p) {
         s.clear();
         norm_channels ch;
         int8_eight<X> v[NV];
-        load_near_rows<decltype(whole)::value>(v, x, (uint32_t)p.ldx, 8 * at, nch, r, R, P);
-        if (active) ch.load(p, c0 + 8 * at, n);
+        load_near_rows<decltype(whole)::value>(v, x, (uint32_t)p.ldx, c, nch, r, R, P);
+        if (active) ch.load(p, c0 + c, n);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (active && r + k * R < P) s.add(v[k]);
+            if (active && r + k * R < P) {
+                if constexpr (decltype(whole)::value) s.add(v[k]);
+                else {
+                    int8_eight<X> own = v[k];
+                    own.shift(twice);
+                    s.add(own);
+                }
+            }
         join_threads<T, true>(l, s, at, r, cvec, R, nch, ng, p.cg, p.eps);
         if (active) {
-            ch.set(p.cg, c0 + 8 * at, n, g0, l.mean, l.m2);
+            ch.set(p.cg, c0 + c, n, g0, l.mean, l.m2);
             const long long row0 = (long long)image * p.P;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
@@ -338,8 +347,8 @@ norm_one_kernel(norm_args p) {
                     const long long row = row0 + r + k * R;
                     float f[8];
                     ch.apply(v[k], p.act, f);
-                    if (p.token_major) store8(p.y, (size_t)row * p.ldy + c0 + 8 * at, f, n, p.out_bf16);
-                    else store8_apart(p.y, c0 + 8 * at, p.ldy, row, f, n, p.out_bf16);
+                    if (p.token_major) store8(p.y, (size_t)row * p.ldy + c0 + c, f, n, p.out_bf16);
+                    else store8_apart(p.y, c0 + c, p.ldy, row, f, n, p.out_bf16);
                 }
         }
         });
@@ -545,20 +554,20 @@ norm_apply_kernel(norm_args p) {
         const int rows = (int)min(p.y_rows, p.P - chunk * p.y_rows);
         const X* x = static_cast<const X*>(p.x) + row0 * p.ldx + c0;
         if constexpr (TOKENS) {
-            const int R = quotient(T, cvec), r = quotient(tid, cvec), at = tid - r * cvec, n = min(8, nch - 8 * at);
+            const int R = quotient(T, cvec), r = quotient(tid, cvec), at = tid - r * cvec, n = min(8, nch), c = max(0, min(8 * at, nch - 8));     // (a last vector that is not whole: the last eight channels, some twice)
             // (the first rows, gamma and beta are on their way while the statistics are joined)
             whole_or_not(nch, [&](auto whole) {
                 constexpr int AHEAD = sizeof(X) == 2 ? 8 : 4;
                 norm_channels ch;
                 int8_eight<X> u[AHEAD];
-                load_rows<decltype(whole)::value>(u, x, p.ldx, 8 * at, nch, r, R, rows);
-                ch.load(p, c0 + 8 * at, n);
+                load_rows<decltype(whole)::value>(u, x, p.ldx, c, nch, r, R, rows);
+                ch.load(p, c0 + c, n);
                 join_parts<T>(p, image, g0, ng, smem, smem + ng);
                 if (r >= R) return;
-                ch.set(p.cg, c0 + 8 * at, n, g0, smem, smem + ng);
-                const size_t to = (size_t)row0 * p.ldy + c0 + 8 * at;
+                ch.set(p.cg, c0 + c, n, g0, smem, smem + ng);
+                const size_t to = (size_t)row0 * p.ldy + c0 + c;
                 for (int pos = r; pos < rows; pos += AHEAD * R) {
-                    if (pos != r) load_rows<decltype(whole)::value>(u, x, p.ldx, 8 * at, nch, pos, R, rows);
+                    if (pos != r) load_rows<decltype(whole)::value>(u, x, p.ldx, c, nch, pos, R, rows);
 #pragma unroll
                     for (int k = 0; k < AHEAD; ++k)
                         if (pos + k * R < rows) {

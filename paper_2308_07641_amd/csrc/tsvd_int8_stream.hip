@@ -1,7 +1,7 @@
 // Products of 8-bit codes (include/tsvd_int8.h) for few tokens: the weights pass once through the matrix unit, straight from memory into operand registers
 // (v_mfma_i32_16x16x64_i8, 16 rows x 16 tokens), and that stream bounds the call.
 //
-// A workgroup owns a run of strips of 16 rows.  Its wavefronts split the contraction (and, where it is short, the strips): a wavefront holds the codes of its part in
+// A workgroup owns a run of strips of 16 rows and up to 64 tokens.  Its wavefronts split the contraction (and, where it is short, the strips): a wavefront holds the codes of its part in
 // registers, KT tiles of 64 indices by NB blocks of 16 tokens, and goes through the strips, and on into the next part, with the tiles of the next two on their way.  The parts
 // meet in LDS as integers, by additions whose order does not matter.  Nothing stands between the launch and the stream but the codes.
 //
@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "tsvd_epilogue.h"
+#include "tsvd_kernels.h"
 
 namespace {
 
@@ -30,7 +31,9 @@ struct stream_args {
     void* y;
     long long ldy;
     long long M;
-    int nkt, strips, N, B;
+    int nkt, strips, N;
+    long long B;
+    int strip_groups;                    // workgroups of a group of tokens (16 NB at most)
     int strips_wg, kw, kw_log2, sw;      // strips of a workgroup; wavefronts along the contraction (a power of two), along the strips
     int token_major, out_bf16;
 };
@@ -53,7 +56,9 @@ int8_stream_kernel(stream_args p) {
     __shared__ float token_scale[16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int ks = wave & (p.kw - 1), sg = wave >> p.kw_log2;
-    const int strip0 = blockIdx.x * p.strips_wg, strips = min(p.strips_wg, p.strips - strip0);
+    const int token_group = blockIdx.x / (unsigned)p.strip_groups, strip0 = (blockIdx.x - token_group * p.strip_groups) * p.strips_wg, strips = min(p.strips_wg, p.strips - strip0);
+    const long long token0 = (long long)token_group * 16 * NB;
+    const int B = (int)min(p.B - token0, 16ll * NB);
     const uint32_t bytes = (uint32_t)strips * p.nkt * 1024;
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.tiles + (size_t)strip0 * p.nkt * 1024), 0, bytes, 0x00020000);
     const int chunk_tiles = p.kw * KT;
@@ -75,8 +80,8 @@ int8_stream_kernel(stream_args p) {
         for (int k = 0; k < KT; ++k) x[u][k] = *reinterpret_cast<const i32x4*>(stage + set * 1024 * KT + place<KT>(i, 4 * k + g));
     };
     const uint32_t stage_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stage;
-    const uint32_t codes_bytes = make ? 0 : (uint32_t)((p.B - 1) * p.ldq) + (uint32_t)((p.N + 15) & ~15);
-    const i32x4 qbuf = buffer_of(p.q, codes_bytes);
+    const uint32_t codes_bytes = make ? 0 : (uint32_t)((B - 1) * p.ldq) + (uint32_t)((p.N + 15) & ~15);
+    const i32x4 qbuf = buffer_of(p.q + token0 * p.ldq, codes_bytes);
     // (tokens and indices beyond the last: zeros, or any codes, where the weights' are zero)
     int voff[KT];
 #pragma unroll
@@ -102,11 +107,11 @@ int8_stream_kernel(stream_args p) {
         for (int k = 0; k < 2 * KT; ++k) {
             v[k].zero();
             if constexpr (ROWS) {
-                if (k * STEP + own < p.B) v[k] = int8_load8(from + (long long)(k * STEP + own) * p.ldq, ks * KT * 64 + 8 * at, p.N);
+                if (k * STEP + own < B) v[k] = int8_load8(from + (long long)(k * STEP + own) * p.ldq, ks * KT * 64 + 8 * at, p.N);
             } else {
                 value e[8];
 #pragma unroll
-                for (int n = 0; n < 8; ++n) e[n] = from[min(i, p.B - 1) + (long long)min((ks * KT + k / 2) * 64 + 16 * g + k % 2 * 8 + n, p.N - 1) * p.ldq];
+                for (int n = 0; n < 8; ++n) e[n] = from[min(i, B - 1) + (long long)min((ks * KT + k / 2) * 64 + 16 * g + k % 2 * 8 + n, p.N - 1) * p.ldq];
 #pragma unroll
                 for (int n = 0; n < 8; ++n) v[k].set(n, e[n]);
             }
@@ -203,14 +208,14 @@ int8_stream_kernel(stream_args p) {
     if constexpr (!make) wait_vmcnt<0>();                            // (nothing may come to LDS after the end)
     __syncthreads();
     // lanes along the rows of a token (token-major y, and single tokens), else along the tokens of a row
-    const int rows = (int)min((long long)strips * 16, p.M - (long long)strip0 * 16), along_rows = p.token_major || p.B == 1;
-    const int inner = along_rows ? rows : p.B, total = rows * p.B;
+    const int rows = (int)min((long long)strips * 16, p.M - (long long)strip0 * 16), along_rows = p.token_major || B == 1;
+    const int inner = along_rows ? rows : B, total = rows * B;
     for (int n = threadIdx.x; n < total; n += blockDim.x) {
         const int o = n / inner, e = n - o * inner, row = along_rows ? e : o, token = along_rows ? o : e;
-        const long long m = (long long)strip0 * 16 + row;
+        const long long m = (long long)strip0 * 16 + row, t = token0 + token;
         const int sum = smem[((row >> 4) * NB + (token >> 4)) * BLOCK + (row & 15) * BLOCK_PITCH + (token & 15)];
-        const float f = int8_result(sum, p.t[m], make ? token_scale[token] : p.s[token], p.bias ? p.bias[m] : 0.f);
-        tsvd_store_y(p.y, p.token_major ? (size_t)token * p.ldy + m : (size_t)m * p.ldy + token, f, p.out_bf16);
+        const float f = int8_result(sum, p.t[m], make ? token_scale[token] : p.s[t], p.bias ? p.bias[m] : 0.f);
+        tsvd_store_y(p.y, p.token_major ? (size_t)t * p.ldy + m : (size_t)m * p.ldy + t, f, p.out_bf16);
     }
 }
 
@@ -223,7 +228,8 @@ struct stream_plan {
 stream_plan plan_of(long long strips, int nkt, long long B, int cus, int most) {
     stream_plan s;
     s.nb = B <= 16 ? 1 : B <= 32 ? 2 : 4;
-    s.strips_wg = (int)std::max<long long>(1, std::min<long long>((strips + cus - 1) / cus, MAX_BLOCKS / s.nb));
+    const long long groups = (B + 16 * s.nb - 1) / (16 * s.nb);
+    s.strips_wg = (int)std::max<long long>(1, std::min<long long>((strips * groups + cus - 1) / cus, MAX_BLOCKS / s.nb));
     s.kt = most;
     s.kw = 1;
     while (s.kw < 16 && s.kw * s.kt < nkt) s.kw *= 2;
@@ -260,8 +266,8 @@ stream_args args_of(const tsvd_int8_problem& p, const stream_plan& s) {
     const tsvd_int8_handle& h = *p.h;
     stream_args a = {};
     a.tiles = h.tiles(), a.nkt = h.nkt, a.strips = (int)h.strips, a.N = (int)h.N, a.t = h.scales(), a.M = h.M;
-    a.s = p.scales, a.B = (int)p.B, a.bias = p.bias, a.y = p.y, a.ldy = p.ldy, a.token_major = p.token_major, a.out_bf16 = p.out_bf16;
-    a.strips_wg = s.strips_wg, a.kw = s.kw, a.sw = s.sw;
+    a.s = p.scales, a.B = p.B, a.bias = p.bias, a.y = p.y, a.ldy = p.ldy, a.token_major = p.token_major, a.out_bf16 = p.out_bf16;
+    a.strips_wg = s.strips_wg, a.strip_groups = (a.strips + s.strips_wg - 1) / s.strips_wg, a.kw = s.kw, a.sw = s.sw;
     while (1 << a.kw_log2 < s.kw) ++a.kw_log2;
     return a;
 }
@@ -278,13 +284,19 @@ hipError_t tsvd_int8_stream_init() {
     return hipSuccess;
 }
 
-bool tsvd_int8_stream_serves(const tsvd_int8_handle&, long long B) { return B <= 64; }
+// Up to 64 tokens; and more, 64 a workgroup, where tiles of rows and tokens would leave most compute units idle over a long contraction: up to two strips for each compute unit.
+// 46 rows of 14336 features, 256 tokens 13.8 us (tiles 23.3), 2048 rows of 4096 8.2 (9.1); of 640 features 5.4 (3.8), four strips each, 4096 rows of 4096, 11.8 (10.0).
+bool tsvd_int8_stream_serves(const tsvd_int8_handle& h, long long B) {
+    if (B <= 64) return true;
+    const long long strips = (h.strips * ((B + 63) / 64) + h.cu_count - 1) / h.cu_count;
+    return strips <= 2 && h.nkt / 2 >= 10 * strips && tsvd_tune("TSVD_INT8_TILE", 0) == 0;
+}
 
 hipError_t tsvd_int8_stream(const tsvd_int8_problem& p, hipStream_t stream) {
     const stream_plan s = plan_of(p.h->strips, p.h->nkt, p.B, p.h->cu_count, CODES_TILES);
     stream_args a = args_of(p, s);
     a.q = reinterpret_cast<const uint8_t*>(p.codes), a.ldq = p.ldq;
-    const int grid = (a.strips + s.strips_wg - 1) / s.strips_wg;
+    const int grid = (int)(a.strip_groups * ((p.B + 16 * s.nb - 1) / (16 * s.nb)));
     return s.nb == 1 ? launch_codes<1>(s.kt, a, grid, stream) : s.nb == 2 ? launch_codes<2>(s.kt, a, grid, stream) : launch_codes<4>(s.kt, a, grid, stream);
 }
 
@@ -297,7 +309,7 @@ hipError_t tsvd_int8_stream_from(const tsvd_int8_problem& p, const void* x, bool
     const stream_plan s = plan_of(p.h->strips, p.h->nkt, p.B, p.h->cu_count, MAKE_TILES);
     stream_args a = args_of(p, s);
     a.q = static_cast<const uint8_t*>(x), a.ldq = ldx;
-    const int grid = (a.strips + s.strips_wg - 1) / s.strips_wg;
+    const int grid = a.strip_groups;
     if (rows) return x_bf16 ? launch_make<uint16_t, true>(s.kt, a, grid, stream) : launch_make<float, true>(s.kt, a, grid, stream);
     return x_bf16 ? launch_make<uint16_t, false>(s.kt, a, grid, stream) : launch_make<float, false>(s.kt, a, grid, stream);
 }

@@ -169,9 +169,13 @@ __device__ __forceinline__ void store8(void* y, size_t at, const float (&f)[8], 
 }
 // ... and in rows of their own (feature-major y)
 __device__ __forceinline__ void store8_apart(void* y, int c0, long long ldy, long long row, const float (&f)[8], int n, int out_bf16) {
+    size_t at = (size_t)c0 * ldy + row;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < n) tsvd_store_y(y, (size_t)(c0 + e) * ldy + row, f[e], out_bf16);
+    for (int e = 0; e < 8; ++e) {
+        if (e < n) tsvd_store_y(y, at, f[e], out_bf16);
+        at += ldy;
+        asm("" : "+v"(at));                              // (eight places held over a loop of rows are registers that the rows need)
+    }
 }
 
 __device__ __forceinline__ uint2 codes_of(const float (&f)[8], float factor) {
@@ -924,7 +928,7 @@ hipError_t rows_form(const norm_args& a, hipStream_t stream) {
     if (a.C <= 2048) return rows(norm_rows_kernel<X, 256, 1, CODES>, 256, a.images, 6);
     if (a.C <= 4096) return rows(norm_rows_kernel<X, 256, 2, CODES>, 256, a.images, 4);
     if (a.C <= 8192) return rows(norm_rows_kernel<X, 512, 2, CODES>, 512, a.images, 2);
-    return rows(norm_rows_kernel<X, 1024, 2, CODES>, 1024, a.images, 1);
+    return rows(norm_rows_kernel<X, 512, 4, CODES>, 512, a.images, 1);      // (1024 lanes of two vectors spill: 2048 rows of 16384 channels 56 us)
 }
 
 template <typename X>

@@ -108,7 +108,8 @@ def test_zeros_tiny_values_and_values_that_are_no_numbers(tsvd, token_major):
 
 # rows, features, tokens
 LAYERS = [(1, 1, 1), (16, 64, 1), (17, 65, 3), (100, 100, 16), (256, 256, 1), (300, 1000, 17), (1000, 2047, 33), (130, 4097, 64), (513, 520, 65), (48, 16385, 5), (33, 131071, 2),
-          (2000, 128, 300), (129, 127, 1025), (4100, 320, 1), (260, 4096, 31), (70, 9216, 130), (5000, 70, 2)]
+          (2000, 128, 300), (129, 127, 1025), (4100, 320, 1), (260, 4096, 31), (70, 9216, 130), (5000, 70, 2),
+          (60, 14381, 471), (1999, 2700, 190), (4000, 5000, 37), (30, 20000, 65)]
 
 
 def layer(rng, M, N):

@@ -892,18 +892,25 @@ void cut_y(norm_args* a, bool token_major) {
     a->y_chunks = up(a->P, a->y_rows);
 }
 
-// One launch: the groups of a workgroup, 0 where it would hold too much.  As few as give every compute unit a workgroup, but 64 bytes of a row at least (single groups of 20 channels, 40
-// bytes: 8 images of 1024 positions, 640 channels, 18.1 us on 256 compute units, 13.5 with pairs of groups on 128).
+// One launch: the groups of a workgroup, 0 where it would hold too much.  As few as give every compute unit a workgroup, down to 16 bytes of a row (8 images of 1024 positions, 640
+// channels in 32 groups, bf16: single groups, 40 bytes, 12.3 us, pairs on half of the compute units 13.8; fp32, whose rows a compute unit holds half as many of: down to 64 bytes
+// in whole vectors, 15.7 us, single groups 17.6), and as few as the registers hold, down to 64 bytes.  Not where a thread would have many positions of less, or few workgroups
+// many (4 images of 4096 positions, 320 channels: 19.8 us, by pieces 17.0; one of 714 positions, 4 groups of 73 channels: 16.1, by pieces 10.3).
 template <typename X>
 int one_launch(const norm_args& a, int T, int rows_of_thread) {
     int gpb = std::min(a.G, T * 8 / a.cg);
     if (gpb < 1 || a.P * a.ldx > INT32_MAX / 4) return 0;       // (places of an image in 32 bits)
     // whole vectors side by side where groups allow it
-    const int unit = whole_groups(a.cg) <= gpb ? whole_groups(a.cg) : 1;
+    const int unit = sizeof(X) == 4 && whole_groups(a.cg) <= gpb ? whole_groups(a.cg) : 1;
     auto rows_with = [&](int groups) { return up(a.P, T / up((long long)groups * a.cg, 8)); };
-    while (gpb > unit && (a.images * up(a.G, gpb) < CUS || rows_with(gpb) > rows_of_thread) &&
-           (long long)std::max(unit, gpb / 2 / unit * unit) * a.cg * (int)sizeof(X) >= 64) gpb = std::max(unit, gpb / 2 / unit * unit);
-    return rows_with(gpb) <= rows_of_thread ? gpb : 0;
+    auto run = [&](int groups) { return (long long)groups * a.cg * (int)sizeof(X); };
+    while (gpb > unit) {
+        const int fewer = std::max(unit, gpb / 2 / unit * unit);
+        if (!(run(fewer) >= (sizeof(X) == 2 ? 16 : 64) && a.images * up(a.G, gpb) < CUS) && !(run(fewer) >= 64 && rows_with(gpb) > rows_of_thread)) break;
+        gpb = fewer;
+    }
+    const long long rows = rows_with(gpb);
+    return rows > rows_of_thread || (rows > 8 && (run(gpb) < 64 || a.images * up(a.G, gpb) < 32)) ? 0 : gpb;
 }
 
 template <typename K>

@@ -2,6 +2,7 @@
 //
 // Codes: q = rne(x 127 / a), a the largest magnitude of the token.  Bound by memory: x once, a byte for each value back; five
 // operations a value (unpacking, the magnitude's two, one fma that multiplies and rounds, its share of the byte permutes).
+// Measured, bf16: 2048 tokens of 9216 features 16 us token-major (3.5 TB/s), 21 us feature-major in slices; 12544 of 512 feature-major, held in registers, 8.3 us; 256 of 4096 4.8 us.
 #include "tsvd_int8.h"
 
 #include <algorithm>
@@ -279,7 +280,8 @@ columns_plan plan_columns(long long B, int N) {
     columns_plan c;
     c.tv = B >= 512 ? 8 : B > 16 ? 2 : 1;
     const long long blocks = (B + 8 * c.tv - 1) / (8 * c.tv), step = 1024 / c.tv;
-    // one launch where a workgroup's registers hold all features and there is a workgroup for every other compute unit, or where there is next to nothing to do
+    // one launch where a workgroup's registers hold all features and there is a workgroup for every other compute unit, or where there is next to nothing to do; slices elsewhere, about
+    // 512 workgroups of them (2048 tokens of 9216 features 21 us, 38 in one launch that reads x twice; 64 of 16384 8 us and 28)
     const bool held = N <= (B >= 4096 ? 4096 : 2048) && B >= 1024;
     const long long slices = std::min<long long>((N + step - 1) / step, std::max<long long>(1, (512 + blocks - 1) / blocks));
     c.slices = held || slices < 2 || B * N <= 8192 ? 1 : (int)slices;

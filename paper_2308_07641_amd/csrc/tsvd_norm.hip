@@ -2,11 +2,14 @@
 //
 // Bound by memory: x once and y once where a workgroup can hold what it normalises, else x twice.  A thread keeps eight neighbouring channels and walks along the
 // positions: sums of x - k and (x - k)^2 for each channel, k being the first value that it meets.  As k is one of the values, the deviations that cancel are
-// part of the result: the sum of squares about the thread's own mean is right to the number of its values times 2^-24, whatever the values are.  Threads, and
-// pieces of an image, are then joined by n (mean - common mean)^2, never by a difference of squares.  Every sum has a fixed order.
+// part of the result: the sum of squares about the thread's own mean is right to the number of its values times 2^-24, whatever the values are.  Threads, and pieces of an
+// image, are then joined as counts, sums and sums of squares in fp64, where what cancels is 2^-53 of the mean's square.  Every sum has a fixed order.
 //
-// Forms: rows (one position and one group: a row in registers), one launch (a workgroup has all positions of an image for some groups), and two launches (statistics
-// of pieces; y, every workgroup joining the pieces that it needs).
+// Forms: rows (one position and one group: a row in registers), one launch (a workgroup has all positions of an image for some groups, or whole images: codes), and two launches
+// (statistics of pieces; y or codes, every workgroup joining the pieces that it needs; x comes a second time, from the memory-side cache where it fits).
+//
+// Measured: 16 images of 16384 positions, 256 channels in 32 groups, bf16: statistics 40 us (3.3 TB/s), y 47 us (5.6 TB/s both ways); 8 of 1024 x 640 in one launch 11.8 us; one of
+// 64 x 320 5.0 us; 2048 rows of 4096 into codes 9 us (2.8 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

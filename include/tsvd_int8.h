@@ -73,7 +73,7 @@ void tsvd_int8_free(tsvd_int8_handle* h);
  * y from codes that are there (several layers that read the same activations share them):
  *   y_dev : [M][B] with ldy >= B (TSVD_FEATURE_MAJOR) or [B][M] with ldy >= M (TSVD_TOKEN_MAJOR), of y_dtype, at any stride and element
  *           alignment.   bias_dev : device fp32 [M] or NULL.
- * TSVD_EINVAL as above; TSVD_EUNSUPPORTED: B > 2^24 or ldq > 2^22. */
+ * TSVD_EINVAL as above, and where the current device is not the one of the handle; TSVD_EUNSUPPORTED: B > 2^24 or ldq > 2^22. */
 tsvd_status tsvd_int8_product(const tsvd_int8_handle* h, const int8_t* codes_dev, int64_t ldq, const float* scales_dev, int64_t B,
                               const float* bias_dev, void* y_dev, tsvd_dtype y_dtype, tsvd_layout y_layout, int64_t ldy, void* stream);
 

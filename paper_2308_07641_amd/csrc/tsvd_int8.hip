@@ -353,6 +353,12 @@ bool bad_layout(int l) { return l != TSVD_FEATURE_MAJOR && l != TSVD_TOKEN_MAJOR
 // One token is a contiguous vector in either layout, whatever its stride means: as one row.
 bool one_row(tsvd_layout layout, int64_t B, int64_t ldx) { return layout == TSVD_TOKEN_MAJOR || (B == 1 && ldx == 1); }
 
+// The weights are where the launch will be.
+bool on_its_device(const tsvd_int8_handle* h) {
+    int device = -1;
+    return hipGetDevice(&device) == hipSuccess && device == h->device;
+}
+
 size_t codes_bytes(const tsvd_int8_handle* h, int64_t B) { return round256((size_t)B * tsvd_int8_row_bytes(h->N)); }
 
 }  // namespace
@@ -448,6 +454,7 @@ extern "C" tsvd_status tsvd_int8_product(const tsvd_int8_handle* h, const int8_t
     if (!h || !scales_dev || !y_dev || B < 1 || bad_dtype(y_dtype) || bad_layout(y_layout)) return TSVD_EINVAL;
     if (bad_codes(codes_dev, ldq, h->N) || ldy < (y_layout == TSVD_TOKEN_MAJOR ? h->M : B)) return TSVD_EINVAL;
     if (B > TSVD_INT8_MAX_B || ldq > TSVD_INT8_MAX_PITCH) return TSVD_EUNSUPPORTED;
+    if (!on_its_device(h)) return TSVD_EINVAL;
     const tsvd_int8_problem p = {h, codes_dev, ldq, scales_dev, B, bias_dev, y_dev, y_dtype == TSVD_BF16, y_layout == TSVD_TOKEN_MAJOR, ldy};
     const hipError_t e = tsvd_int8_stream_serves(*h, B) ? tsvd_int8_stream(p, static_cast<hipStream_t>(stream)) : tsvd_int8_gemm(p, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? TSVD_OK : e == hipErrorNotSupported ? TSVD_EUNSUPPORTED : TSVD_EDEVICE;
@@ -470,7 +477,7 @@ extern "C" tsvd_status tsvd_int8_forward(const tsvd_int8_handle* h, const void* 
     if (!h || !x_dev || !y_dev || B < 1 || bad_dtype(x_dtype) || bad_layout(x_layout) || bad_dtype(y_dtype) || bad_layout(y_layout)) return TSVD_EINVAL;
     if (ldx < (x_layout == TSVD_TOKEN_MAJOR ? h->N : B) || ldy < (y_layout == TSVD_TOKEN_MAJOR ? h->M : B)) return TSVD_EINVAL;
     if (B > TSVD_INT8_MAX_B) return TSVD_EUNSUPPORTED;
-    if (bad_workspace(workspace, workspace_bytes, tsvd_int8_workspace_bytes(h, B, x_dtype, x_layout))) return TSVD_EINVAL;
+    if (bad_workspace(workspace, workspace_bytes, tsvd_int8_workspace_bytes(h, B, x_dtype, x_layout)) || !on_its_device(h)) return TSVD_EINVAL;
     if (made_in_launch(h, B)) {
         const tsvd_int8_problem p = {h, nullptr, 0, nullptr, B, bias_dev, y_dev, y_dtype == TSVD_BF16, y_layout == TSVD_TOKEN_MAJOR, ldy};
         return tsvd_int8_stream_from(p, x_dev, x_dtype == TSVD_BF16, one_row(x_layout, B, ldx), ldx, static_cast<hipStream_t>(stream)) == hipSuccess ? TSVD_OK : TSVD_EDEVICE;

@@ -323,11 +323,11 @@ PyObject* codes_and_scales(y_ref& codes, y_ref& scales) {
 void check_codes(const codes_view& c, int64_t B, int64_t N, const char* text) {
     if (c.B != B || c.N != N) raise(PyExc_ValueError, text);
 }
-// A single row of codes: only what its 16-byte pieces need is known to be there.
-void check_single_row(PyObject* o) {
-    const at::Tensor& c = THPVariable_Unpack(o);
-    const int64_t left = (int64_t)c.storage().nbytes() - c.storage_offset();
-    if (c.size(0) == 1 && left < (c.size(1) + 15) / 16 * 16) raise(PyExc_ValueError, "codes: a row needs room up to the next multiple of 16 bytes");
+// Codes are read and written in pieces of 16 bytes: the last row's last one has to be there.
+void check_room(PyObject* o, const codes_view& c) {
+    const at::Tensor& t = THPVariable_Unpack(o);
+    const int64_t left = (int64_t)t.storage().nbytes() - t.storage_offset();
+    if (c.B > 0 && c.N > 0 && c.ldq >= 0 && left < (c.B - 1) * c.ldq + (c.N + 15) / 16 * 16) raise(PyExc_ValueError, "codes: every row needs room up to the next multiple of 16 bytes");
 }
 
 // int8_quantize(x, x_layout, codes, scales, workspace, stream)
@@ -347,7 +347,7 @@ PyObject* py_int8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!codes.p || !scales.p) throw failed();
         const codes_view c = codes_of(codes.p);
         check_codes(c, B, N, "codes must be [B,N]");
-        check_single_row(codes.p);
+        check_room(codes.p, c);
         same_device(THPVariable_Unpack(codes.p), x, "codes must live on x's device");
         float* s = const_cast<float*>(floats_of(scales.p, B, x, "scales must be a contiguous float32 GPU tensor [B] on x's device"));
         const size_t need = tsvd_int8_quantize_workspace_bytes(B, N, xl);
@@ -412,7 +412,7 @@ PyObject* py_int8_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor& q = THPVariable_Unpack(a[1]);
         const c10::DeviceGuard device(q.device());
         if (c.N != h.N) raise(PyExc_ValueError, "codes do not have N features");
-        check_single_row(a[1]);
+        check_room(a[1], c);
         const tsvd_layout yl = (tsvd_layout)integer(a[6]);
         const int64_t yd = integer(a[5]);
         const bool ytm = yl == TSVD_TOKEN_MAJOR;
@@ -478,7 +478,7 @@ PyObject* py_group_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
             if (!codes.p || !scales.p) throw failed();
             const codes_view c = codes_of(codes.p);
             check_codes(c, images * P, C, "codes must be [images * positions,C]");
-            check_single_row(codes.p);
+            check_room(codes.p, c);
             same_device(THPVariable_Unpack(codes.p), x, "codes must live on x's device");
             float* s = const_cast<float*>(floats_of(scales.p, images * P, x, "scales must be a contiguous float32 GPU tensor [images * positions] on x's device"));
             const workspace_view ws = scratch_of(workspace, need, x, &made);

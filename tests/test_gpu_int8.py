@@ -327,3 +327,26 @@ def test_refusals(tsvd):
     with pytest.raises(tsvd.TsvdError):
         tsvd.tsvd_int8_forward(h, x, x_layout=tsvd.TSVD_TOKEN_MAJOR)
     tsvd.tsvd_int8_free(h2)
+
+
+def test_codes_need_room_for_whole_pieces(tsvd):
+    """Rows of codes are read and written 16 bytes at a time: a view whose last row ends sooner is refused, one that ends there is taken."""
+    import torch
+    N, B, ldq = 37, 3, 64
+    h = tsvd.tsvd_int8_pack(torch.ones(5, N, dtype=torch.int8, device="cuda:0"), torch.ones(5, device="cuda:0"))
+    x = torch.randn(B, N, device="cuda:0")
+    for short in (1, 11):
+        buf = torch.zeros((B - 1) * ldq + 48 - short, dtype=torch.int8, device="cuda:0")
+        q = buf.as_strided((B, N), (ldq, 1))
+        with pytest.raises(ValueError):
+            tsvd.tsvd_int8_quantize(x, codes=q)
+        with pytest.raises(ValueError):
+            tsvd.tsvd_int8_product(h, q, torch.ones(B, device="cuda:0"))
+        with pytest.raises(ValueError):
+            tsvd.tsvd_group_norm_int8(x, 1, codes=q)
+    q = torch.zeros((B - 1) * ldq + 48, dtype=torch.int8, device="cuda:0").as_strided((B, N), (ldq, 1))
+    q, s = tsvd.tsvd_int8_quantize(x, codes=q)
+    want, scales = tsvd.tsvd_int8_quantize(x)
+    assert torch.equal(q, want) and torch.equal(s, scales)
+    assert torch.equal(tsvd.tsvd_int8_product(h, q, s), tsvd.tsvd_int8_product(h, want, scales))
+    tsvd.tsvd_int8_free(h)

@@ -280,9 +280,10 @@ columns_plan plan_columns(long long B, int N) {
     columns_plan c;
     c.tv = B >= 512 ? 8 : B > 16 ? 2 : 1;
     const long long blocks = (B + 8 * c.tv - 1) / (8 * c.tv), step = 1024 / c.tv;
-    // one launch where a workgroup's registers hold all features and there is a workgroup for every other compute unit, or where there is next to nothing to do; slices elsewhere, about
-    // 512 workgroups of them (2048 tokens of 9216 features 21 us, 38 in one launch that reads x twice; 64 of 16384 8 us and 28)
-    const bool held = N <= (B >= 4096 ? 4096 : 2048) && B >= 1024;
+    // one launch where a workgroup's registers hold all features, or where there is next to nothing to do; slices elsewhere, about 512 workgroups of them (2048 tokens of 9216 features
+    // 21 us, 38 in one launch that reads x twice; 64 of 16384 8 us and 28), and for few tokens whose rows do not stand on 16 bytes (4096 features: 197 tokens 11.5 us, in one launch 14.5;
+    // 256 tokens 7.7 and 7.6, 3000 tokens 21.2 and 16.9)
+    const bool held = N <= 2048 || (N <= 4096 && (B <= 64 || B >= 1024 || B % 8 == 0));
     const long long slices = std::min<long long>((N + step - 1) / step, std::max<long long>(1, (512 + blocks - 1) / blocks));
     c.slices = held || slices < 2 || B * N <= 8192 ? 1 : (int)slices;
     c.rows = (int)(((N + c.slices - 1) / c.slices + step - 1) / step * step);
@@ -323,16 +324,20 @@ hipError_t quantize(const X* x, bool token_major, long long B, int N, long long 
         auto columns = [&](auto kernel, int threads, int tokens) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)((B + tokens - 1) / tokens)), dim3(threads), 0, stream, x, ldx, B, N, q, ldq, s);
         };
-        // 64 bytes of a row (bf16) for each workgroup where that leaves one for most compute units, else fewer tokens
+        // 64 bytes of a row (bf16) for each workgroup where that leaves one for most compute units, else fewer tokens (3000 tokens, 2048 features: 32 bytes 9.5 us, 16 bytes 10.9; 3000 of
+        // 4096, which only sixteen bytes' worth fits registers of: 16.9)
         if (B >= 4096) {
             if (N <= 512) columns(int8_quantize_columns_kernel<X, 256, 4, 2>, 256, 32);
             else if (N <= 2048) columns(int8_quantize_columns_kernel<X, 1024, 4, 2>, 1024, 32);
             else columns(int8_quantize_columns_kernel<X, 1024, 4, sizeof(X) == 2 ? 4 : 0>, 1024, 32);
-        } else if (B >= 1024) {
+        } else if (B >= 1024 && N <= 2048) {
             if (N <= 1024) columns(int8_quantize_columns_kernel<X, 256, 2, 2>, 256, 16);
             else columns(int8_quantize_columns_kernel<X, 1024, 2, 2>, 1024, 16);
         } else {
-            if (N <= 2048) columns(int8_quantize_columns_kernel<X, 256, 1, 2>, 256, 8);
+            if (N <= 512) columns(int8_quantize_columns_kernel<X, 128, 1, 1>, 128, 8);
+            else if (N <= 1024) columns(int8_quantize_columns_kernel<X, 256, 1, 1>, 256, 8);
+            else if (N <= 2048) columns(int8_quantize_columns_kernel<X, 512, 1, 1>, 512, 8);
+            else if (N <= 4096) columns(int8_quantize_columns_kernel<X, 512, 1, 2>, 512, 8);
             else columns(int8_quantize_columns_kernel<X, 1024, 1, 0>, 1024, 8);
         }
     }

@@ -55,7 +55,8 @@ def values(rng, B, N, spread=True):
     return x
 
 
-SHAPES = [(4100, 100), (4100, 700), (4097, 2100), (1030, 1025), (1025, 4100), (1024, 8200), (300, 130), (9, 9000), (1, 1), (1, 15), (3, 16), (2, 17), (5, 511), (4, 513), (3, 1025), (33, 100), (2, 2049), (3, 4097), (1, 8193), (2, 16385), (2, 131071), (70, 260)]
+SHAPES = [(4100, 100), (4100, 700), (4097, 2100), (1030, 1025), (1025, 4100), (1024, 8200), (300, 130), (9, 9000), (1, 1), (1, 15), (3, 16), (2, 17), (5, 511), (4, 513), (3, 1025), (33, 100), (2, 2049), (3, 4097), (1, 8193), (2, 16385), (2, 131071), (70, 260),
+          (50, 2000), (64, 4096), (61, 3999), (1000, 1700), (1000, 3500), (600, 500), (200, 900), (197, 3000), (40, 16384)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

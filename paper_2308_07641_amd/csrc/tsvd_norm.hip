@@ -387,19 +387,20 @@ norm_one_int8_kernel(norm_args p) {
             for (int k = 0; k < NV; ++k)
                 if (active && r + k * R < P) s.add(v[k]);
             join_threads<T, true>(l, s, at, r, cvec, R, C, ng, p.cg, p.eps);
-            if (active) ch.set(p.cg, 8 * at, n, 0, l.mean, l.m2);
-            if (active)
+            float f[NV][8];
+            if (active) {
+                ch.set(p.cg, 8 * at, n, 0, l.mean, l.m2);
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
                     if (r + k * R < P) {
-                        float f[8];
-                        ch.apply(v[k], p.act, f);
+                        ch.apply(v[k], p.act, f[k]);
                         uint32_t top = 0;
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            if (e < n) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+                            if (e < n) top = max(top, __float_as_uint(f[k][e]) & 0x7FFFFFFFu);
                         tops[k * T + tid] = top;
                     }
+            }
             __syncthreads();
             const int log = lanes_log2(P, T), lane = tid & ((1 << log) - 1);
             for (int pos = tid >> log; pos < P; pos += T >> log) {
@@ -416,11 +417,7 @@ norm_one_int8_kernel(norm_args p) {
             if (active)
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
-                    if (r + k * R < P) {
-                        float f[8];
-                        ch.apply(v[k], p.act, f);
-                        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + ((long long)image * P + r + k * R) * p.ldy + 8 * at) = codes_of(f, factors[r + k * R]);
-                    }
+                    if (r + k * R < P) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + ((long long)image * P + r + k * R) * p.ldy + 8 * at) = codes_of(f[k], factors[r + k * R]);
         });
         __syncthreads();
     }
@@ -973,9 +970,8 @@ template <typename X>
 hipError_t norm_codes(norm_args a, hipStream_t stream) {
     if (a.P == 1 && a.G == 1 && a.C <= 16384) return rows_form<X, true>(a, stream);
     const long long cvec = up(a.C, 8);
-    // Whole images, positions of a thread at most 1, 4 or 8.  Eight leave a compute unit one workgroup: for 64 to 512 images (320 channels, 64 positions: 256 images 12.1 us, 18.6 by
-    // pieces; 2695 images 114 us, 98.5 by pieces; one of 49 positions and 512 channels 11.3 us, 9.8 by pieces), and over 512 channels, whose codes by pieces take more wavefronts
-    // a row or read x twice more (16 positions of 1280 channels: one image 10.5 us and 15.0, 2695 images 110 us and 190).
+    // Whole images, positions of a thread at most 1, 4 or 8.  Against pieces, bf16: 49 positions of 512 channels, one image 9.8 us and 9.6, 2695 images 106 and 102; 40 of 400 in 4
+    // groups 9.0 and 10.1, 91 and 107; 16 of 1280, which pieces read in rows of four wavefronts, 9.0 and 15.0, 96 and 190.
     size_t lds;
     auto whole_images = [&](int T, int NV) {
         const long long R = T / cvec, rows = R ? up(a.P, R) : NV + 1, pieces = sizeof(norm_piece) * R * (cvec + a.G);
@@ -986,7 +982,7 @@ hipError_t norm_codes(norm_args a, hipStream_t stream) {
     if (whole_images(256, 4)) return launch(norm_one_int8_kernel<X, 256, 4>, a.images, 256, lds, stream, a);
     if (whole_images(512, 1)) return launch(norm_one_int8_kernel<X, 512, 1>, a.images, 512, lds, stream, a);
     if (whole_images(1024, 1)) return launch(norm_one_int8_kernel<X, 1024, 1>, a.images, 1024, lds, stream, a);
-    if (((a.images >= 64 && a.images <= 512) || a.C > 512) && whole_images(512, 8)) return launch(norm_one_int8_kernel<X, 512, 8>, a.images, 512, lds, stream, a);
+    if (whole_images(512, 8)) return launch(norm_one_int8_kernel<X, 512, 8>, a.images, 512, lds, stream, a);
     const hipError_t e = statistics<X>(a, stream);
     if (e != hipSuccess) return e;
     lds = 8 * (size_t)a.G;

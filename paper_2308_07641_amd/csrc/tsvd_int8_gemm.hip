@@ -422,17 +422,20 @@ hipError_t allow() {
 }
 
 // The tiles, and what one takes a compute unit (us, all of them busy): to begin and store it (bf16, fp32), for each stage of 128 indices.  Fitted to the times of all five kinds on
-// 256 CUs for 170 sizes (64 to 40000 rows, 64 to 16384 features, 65 to 16384 tokens, both types and layouts): the kind that they choose takes 0.6% longer than the quickest, in the
-// mean, and 22% at most.  Two workgroups of a compute unit take twice as long as one, so only the number of tiles for each counts.
+// 256 CUs for 170 sizes (64 to 40000 rows, 64 to 16384 features, 65 to 16384 tokens, both types and layouts): the kind that they choose takes 0.4% longer than the quickest, in the
+// mean, and 16% at most.  Two workgroups of a compute unit take twice as long as one, so only the number of tiles for each counts.
 enum { TILE_64 = 1, TILE_128x64, TILE_128, TILE_256x128, TILE_256 };
 constexpr struct {
     int rows, tokens;
     double begin, begin_f32, stage;
-} tile_costs[] = {{}, {64, 64, 0.6, 0.8, 0.18}, {128, 64, 2.7, 3.2, 0.33}, {128, 128, 2.1, 2.6, 0.44}, {256, 128, 7.2, 8.6, 0.74}, {256, 256, 6.3, 10.4, 1.32}};
+} tile_costs[] = {{}, {64, 64, 0.44, 0.67, 0.19}, {128, 64, 2.3, 2.3, 0.33}, {128, 128, 2.1, 2.7, 0.44}, {256, 128, 9.2, 9.9, 0.7}, {256, 256, 6.3, 11.1, 1.32}};
 
-hipError_t launch(int tile, const gemm8_args& a, hipStream_t stream) {
+long long up(long long v, long long m) { return (v + m - 1) / m; }
+hipError_t launch(int tile, const gemm8_args& a, int cus, hipStream_t stream) {
     switch (tile) {
-        case TILE_64: return launch<1, 1, 4, 0>(a, stream);
+        // (two stages let five workgroups share a compute unit, four hide more of one's latency: 104576 tokens, 273 rows of 128 features 30 us and 43; 696 tokens, 320 rows of 15296
+        // 60 us and 26)
+        case TILE_64: return up(a.M, 64) * up(a.B, 64) > cus ? launch<1, 1, 2, 0>(a, stream) : launch<1, 1, 4, 0>(a, stream);
         case TILE_128x64: return launch<2, 1, 4, 8>(a, stream);
         case TILE_128: return launch<2, 2, 4, 8>(a, stream);
         case TILE_256x128: return launch<4, 2, 4, 8>(a, stream);
@@ -440,7 +443,6 @@ hipError_t launch(int tile, const gemm8_args& a, hipStream_t stream) {
     }
     return hipErrorInvalidValue;
 }
-long long up(long long v, long long m) { return (v + m - 1) / m; }
 // The kind that takes the least time by these figures.
 int cheapest(long long rows, long long B, int stages, bool f32, int cus) {
     int best = 0;
@@ -456,7 +458,8 @@ int cheapest(long long rows, long long B, int stages, bool f32, int cus) {
 }  // namespace
 
 hipError_t tsvd_int8_gemm_init() {
-    hipError_t e = allow<1, 1, 4, 0>();
+    hipError_t e = allow<1, 1, 2, 0>();
+    if (e == hipSuccess) e = allow<1, 1, 4, 0>();
     if (e == hipSuccess) e = allow<2, 1, 4, 8>();
     if (e == hipSuccess) e = allow<2, 2, 4, 8>();
     if (e == hipSuccess) e = allow<4, 2, 4, 8>();
@@ -470,5 +473,5 @@ hipError_t tsvd_int8_gemm(const tsvd_int8_problem& p, hipStream_t stream) {
     a.tiles = h.tiles(), a.nkt = h.nkt, a.strips = (int)h.strips, a.N = (int)h.N, a.t = h.scales(), a.M = h.M;
     a.q = reinterpret_cast<const uint8_t*>(p.codes), a.ldq = p.ldq, a.s = p.scales, a.B = p.B;
     a.bias = p.bias, a.y = p.y, a.ldy = p.ldy, a.token_major = p.token_major, a.out_bf16 = p.out_bf16;
-    return launch(tsvd_tune("TSVD_INT8_TILE", cheapest(h.M, p.B, h.nkt / 2, !p.out_bf16, h.cu_count)), a, stream);
+    return launch(tsvd_tune("TSVD_INT8_TILE", cheapest(h.M, p.B, h.nkt / 2, !p.out_bf16, h.cu_count)), a, h.cu_count, stream);
 }

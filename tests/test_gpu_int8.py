@@ -158,7 +158,7 @@ def test_layer_against_64_bits(tsvd, M, N, B):
 
 
 @pytest.mark.parametrize("tile", [1, 2, 3, 4, 5])
-@pytest.mark.parametrize("M,N,B", [(64, 128, 65), (65, 64, 66), (257, 385, 130), (300, 1000, 257), (1000, 2049, 100), (513, 130, 600), (37, 4100, 71)])
+@pytest.mark.parametrize("M,N,B", [(64, 128, 65), (65, 64, 66), (257, 385, 130), (300, 1000, 257), (1000, 2049, 100), (513, 130, 600), (37, 4100, 71), (1100, 300, 1090)])
 def test_every_tile_gives_the_same_bits(tsvd, M, N, B, tile):
     """Every kind of tile, ragged in all three sizes (stages 1 to 33, odd and even), both layouts and types, against 64 bits; the sums are whole numbers and the
     rest the same three roundings, so the kinds agree bit for bit."""

@@ -938,11 +938,19 @@ hipError_t rows_form(const norm_args& a, hipStream_t stream) {
     return rows(norm_rows_kernel<X, 512, 4, CODES>, 512, a.images, 1);      // (1024 lanes of two vectors spill: 2048 rows of 16384 channels 56 us)
 }
 
+// LDS of workgroups of T threads with gpb groups each, the last of an image maybe fewer: that one has more rows of threads, and can have more pieces.
+size_t groups_lds(const norm_args& a, int T) {
+    auto bytes = [&](int groups) {
+        const int cvec = (int)up((long long)groups * a.cg, 8);
+        return norm_lds::bytes(groups, T / cvec, cvec);
+    };
+    return std::max(bytes(a.gpb), bytes(a.G - (a.nblk - 1) * a.gpb));
+}
+
 template <typename X>
 hipError_t statistics(const norm_args& a, hipStream_t stream) {
     if (a.gpb == 0) return launch(norm_stats_wide_kernel<X>, a.images * a.G * a.chunks, 256, 0, stream, a);
-    const int cvec = (int)up((long long)a.gpb * a.cg, 8);
-    return launch(norm_stats_kernel<X>, a.images * a.nblk * a.chunks, 256, norm_lds::bytes(a.gpb, 256 / cvec, cvec), stream, a);
+    return launch(norm_stats_kernel<X>, a.images * a.nblk * a.chunks, 256, groups_lds(a, 256), stream, a);
 }
 
 template <typename X>
@@ -954,8 +962,7 @@ hipError_t norm(norm_args a, hipStream_t stream) {
         if (!gpb || (T == 64 && gpb < a.G)) continue;
         norm_args b = a;
         b.gpb = gpb, b.nblk = (int)up(a.G, gpb);
-        const int cvec = (int)up((long long)gpb * a.cg, 8);
-        const size_t lds = norm_lds::bytes(gpb, T / cvec, cvec);
+        const size_t lds = groups_lds(b, T);
         if (T == 64) return launch(norm_one_kernel<X, 64, 8>, b.images * b.nblk, T, lds, stream, b);
         return T == 256 ? launch(norm_one_kernel<X, 256, 8>, b.images * b.nblk, T, lds, stream, b) : launch(norm_one_kernel<X, 512, 16>, b.images * b.nblk, T, lds, stream, b);
     }

@@ -75,7 +75,7 @@ SHAPES = [(1, 1, 1, 1), (1, 1, 8, 8), (2, 1, 96, 1), (3, 1, 100, 4), (1, 64, 320
           (3, 130, 96, 1), (2, 40, 520, 8), (1, 5000, 40, 8), (1, 4, 2048, 1024), (1, 300, 1000, 1),
           (70, 11, 100, 4), (65, 30, 33, 11), (9, 1, 2832, 8), (3, 1, 9000, 9), (2, 3000, 72, 9), (2, 2000, 200, 2), (3, 900, 65, 5), (1, 5000, 8, 2),
           (700, 3, 40, 8), (1100, 1, 72, 9), (600, 4, 320, 32), (2, 700, 60, 4), (2, 900, 130, 13), (2, 600, 300, 4), (2, 300, 700, 7), (3, 90, 1500, 4), (2, 70, 3001, 1), (1, 30, 6000, 8),
-          (5, 1, 5000, 8), (2, 16306, 64, 64), (600, 9, 67, 1), (3, 1, 16001, 1), (100, 40, 330, 33), (8, 500, 64, 8), (4, 777, 294, 21), (1, 714, 292, 4), (2, 300, 45, 5)]
+          (5, 1, 5000, 8), (2, 16306, 64, 64), (600, 9, 67, 1), (3, 1, 16001, 1), (100, 40, 330, 33), (8, 500, 64, 8), (4, 777, 294, 21), (1, 714, 292, 4), (2, 300, 45, 5), (1, 1530, 1984, 64), (100, 300, 217, 7), (2, 3000, 217, 7), (9, 700, 198, 22)]
 
 
 def params(rng, C, which):

@@ -84,6 +84,10 @@ int tsvd_tuning_thin_last(void);
  * taken again because the shifts did not hold. */
 void tsvd_tuning_transition_shifts(int* kept, int* again);
 
+/* The features that the one launch holds which makes the codes of B tokens of N features of feature-major x (tsvd_int8_quantize): 0 any number, as it reads x twice; -1 where there
+ * are two launches, over slices of the features. */
+int tsvd_tuning_int8_columns(int64_t B, int64_t N, tsvd_dtype x_dtype);
+
 /* Copies the phase timestamps ([workgroups][16] 100 MHz ticks) of the last launch of a handle packed with
  * TSVD_CLOCKS = 1 to the host.  Returns 0 on success. */
 int tsvd_tuning_read_clocks(const tsvd_handle* h, long long* out, int workgroups);

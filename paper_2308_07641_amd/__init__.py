@@ -12,5 +12,5 @@ from .tsvd import (  # noqa: F401
     TSVD_ACT_NONE, TSVD_ACT_RELU, TSVD_ACT_SILU, TSVD_ACT_GELU, Int8Handle,
     tsvd_int8_row_bytes, tsvd_int8_quantize_workspace_bytes, tsvd_int8_quantize, tsvd_int8_packed_bytes, tsvd_int8_pack, tsvd_int8_info, tsvd_int8_workspace_bytes, tsvd_int8_forward, tsvd_int8_product, tsvd_int8_free,
     tsvd_group_norm_workspace_bytes, tsvd_group_norm, tsvd_group_norm_int8,
-    tsvd_tuning_set, tsvd_tuning_reset, tsvd_tuning_forward_stages, tsvd_tuning_tile_shapes, tsvd_tuning_one_launch, tsvd_tuning_split_tiles, tsvd_tuning_tiles_by_xcd, tsvd_tuning_thin_shares, tsvd_tuning_thin_last, tsvd_tuning_transition_shifts, tsvd_tuning_read_clocks,
+    tsvd_tuning_set, tsvd_tuning_reset, tsvd_tuning_forward_stages, tsvd_tuning_tile_shapes, tsvd_tuning_one_launch, tsvd_tuning_split_tiles, tsvd_tuning_tiles_by_xcd, tsvd_tuning_thin_shares, tsvd_tuning_thin_last, tsvd_tuning_transition_shifts, tsvd_tuning_int8_columns, tsvd_tuning_read_clocks,
 )

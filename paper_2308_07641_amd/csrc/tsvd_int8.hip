@@ -9,6 +9,7 @@
 #include <new>
 #include <type_traits>
 
+#include "../../include/tsvd_tuning.h"
 #include "tsvd_scratch.h"
 
 namespace {
@@ -291,6 +292,31 @@ columns_plan plan_columns(long long B, int N) {
     return c;
 }
 
+// One launch for feature-major x: threads of a workgroup, vectors of eight tokens side by side, passes held in registers (0: a loop), and the features that those hold.
+template <int T_, int TV_, int PASSES_>
+struct columns_form {
+    static constexpr int T = T_, TV = TV_, PASSES = PASSES_, FEATURES = PASSES * 4 * T / TV;
+};
+// 64 bytes of a row (bf16) for each workgroup where that leaves one for most compute units, else fewer tokens (3000 tokens, 2048 features: 32 bytes 9.5 us, 16 bytes 10.9; 3000 of
+// 4096, which only sixteen bytes' worth fits registers of: 16.9).  Beyond 4096 features nothing holds x: the loop.
+template <typename X, typename F>
+auto with_columns_form(long long B, int N, F&& f) {
+    constexpr int WIDEST = sizeof(X) == 2 ? 4 : 0;               // (fp32 values of four passes are 128 registers of a lane, all that 1024 lanes have)
+    if (B >= 4096) {
+        if (N <= 512) return f(columns_form<256, 4, 2>());
+        if (N <= 2048) return f(columns_form<1024, 4, 2>());
+        if (N <= 4096) return f(columns_form<1024, 4, WIDEST>());
+        return f(columns_form<1024, 4, 0>());
+    }
+    if (B >= 1024 && N <= 1024) return f(columns_form<256, 2, 2>());
+    if (B >= 1024 && N <= 2048) return f(columns_form<1024, 2, 2>());
+    if (N <= 512) return f(columns_form<128, 1, 1>());
+    if (N <= 1024) return f(columns_form<256, 1, 1>());
+    if (N <= 2048) return f(columns_form<512, 1, 1>());
+    if (N <= 4096) return f(columns_form<512, 1, 2>());
+    return f(columns_form<1024, 1, 0>());
+}
+
 template <typename X>
 hipError_t quantize(const X* x, bool token_major, long long B, int N, long long ldx, uint8_t* q, long long ldq, float* s, uint32_t* tops, hipStream_t stream) {
     if (token_major) {
@@ -321,25 +347,12 @@ hipError_t quantize(const X* x, bool token_major, long long B, int N, long long 
             };
             return c.tv == 8 ? sliced(std::integral_constant<int, 8>()) : c.tv == 2 ? sliced(std::integral_constant<int, 2>()) : sliced(std::integral_constant<int, 1>());
         }
-        auto columns = [&](auto kernel, int threads, int tokens) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)((B + tokens - 1) / tokens)), dim3(threads), 0, stream, x, ldx, B, N, q, ldq, s);
-        };
-        // 64 bytes of a row (bf16) for each workgroup where that leaves one for most compute units, else fewer tokens (3000 tokens, 2048 features: 32 bytes 9.5 us, 16 bytes 10.9; 3000 of
-        // 4096, which only sixteen bytes' worth fits registers of: 16.9)
-        if (B >= 4096) {
-            if (N <= 512) columns(int8_quantize_columns_kernel<X, 256, 4, 2>, 256, 32);
-            else if (N <= 2048) columns(int8_quantize_columns_kernel<X, 1024, 4, 2>, 1024, 32);
-            else columns(int8_quantize_columns_kernel<X, 1024, 4, sizeof(X) == 2 ? 4 : 0>, 1024, 32);
-        } else if (B >= 1024 && N <= 2048) {
-            if (N <= 1024) columns(int8_quantize_columns_kernel<X, 256, 2, 2>, 256, 16);
-            else columns(int8_quantize_columns_kernel<X, 1024, 2, 2>, 1024, 16);
-        } else {
-            if (N <= 512) columns(int8_quantize_columns_kernel<X, 128, 1, 1>, 128, 8);
-            else if (N <= 1024) columns(int8_quantize_columns_kernel<X, 256, 1, 1>, 256, 8);
-            else if (N <= 2048) columns(int8_quantize_columns_kernel<X, 512, 1, 1>, 512, 8);
-            else if (N <= 4096) columns(int8_quantize_columns_kernel<X, 512, 1, 2>, 512, 8);
-            else columns(int8_quantize_columns_kernel<X, 1024, 1, 0>, 1024, 8);
-        }
+        return with_columns_form<X>(B, N, [&](auto form) {
+            typedef decltype(form) F;
+            if (F::PASSES && N > F::FEATURES) return hipErrorInvalidValue;      // (a rule that is wrong: nothing is launched)
+            hipLaunchKernelGGL((int8_quantize_columns_kernel<X, F::T, F::TV, F::PASSES>), dim3((unsigned)((B + 8 * F::TV - 1) / (8 * F::TV))), dim3(F::T), 0, stream, x, ldx, B, N, q, ldq, s);
+            return hipGetLastError();
+        });
     }
     return hipGetLastError();
 }
@@ -374,6 +387,12 @@ extern "C" size_t tsvd_int8_quantize_workspace_bytes(int64_t B, int64_t N, tsvd_
     if (x_layout != TSVD_FEATURE_MAJOR || B < 1 || N < 1 || B > TSVD_INT8_MAX_B || N > TSVD_INT8_MAX_N) return 0;
     const columns_plan c = plan_columns(B, (int)N);
     return c.slices > 1 ? round256((size_t)c.slices * B * 4) : 0;
+}
+
+extern "C" int tsvd_tuning_int8_columns(int64_t B, int64_t N, tsvd_dtype x_dtype) {
+    if (B < 1 || N < 1 || B > TSVD_INT8_MAX_B || N > TSVD_INT8_MAX_N || bad_dtype(x_dtype) || plan_columns(B, (int)N).slices > 1) return -1;
+    auto features = [](auto form) { return decltype(form)::FEATURES; };
+    return x_dtype == TSVD_BF16 ? with_columns_form<uint16_t>(B, (int)N, features) : with_columns_form<float>(B, (int)N, features);
 }
 
 extern "C" tsvd_status tsvd_int8_quantize(const void* x_dev, tsvd_dtype x_dtype, tsvd_layout x_layout, int64_t B, int64_t N, int64_t ldx,

@@ -55,6 +55,7 @@ _PROTOTYPES = {
     "tsvd_tuning_thin_shares": (ctypes.c_int, [_i64, _i64, ctypes.c_int, ctypes.c_int, ctypes.c_int]),
     "tsvd_tuning_thin_last": (ctypes.c_int, []),
     "tsvd_tuning_transition_shifts": (None, [ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int)]),
+    "tsvd_tuning_int8_columns": (ctypes.c_int, [_i64, _i64, ctypes.c_int]),
     "tsvd_tuning_read_clocks": (ctypes.c_int, [_vp, _vp, ctypes.c_int]),
     "tsvd_ternarize": (ctypes.c_int, [_vp, _i64, _i64, _i64, ctypes.c_double, _vp, _i64, _vp, _vp]),
     "tsvd_fit_scales_workspace": (_sz, [_i64]),
@@ -355,6 +356,10 @@ def tsvd_tuning_transition_shifts():
     kept, again = ctypes.c_int(0), ctypes.c_int(0)
     load_library().tsvd_tuning_transition_shifts(ctypes.byref(kept), ctypes.byref(again))
     return kept.value, again.value
+
+
+def tsvd_tuning_int8_columns(B: int, N: int, x_dtype: int) -> int:
+    return int(load_library().tsvd_tuning_int8_columns(B, N, x_dtype))
 
 
 def tsvd_tuning_read_clocks(h: Handle, workgroups: int) -> np.ndarray:

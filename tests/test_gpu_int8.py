@@ -351,3 +351,25 @@ def test_codes_need_room_for_whole_pieces(tsvd):
     assert torch.equal(q, want) and torch.equal(s, scales)
     assert torch.equal(tsvd.tsvd_int8_product(h, q, s), tsvd.tsvd_int8_product(h, want, scales))
     tsvd.tsvd_int8_free(h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,N", [(32704, 4100), (32705, 4097), (32768, 4096), (33001, 9216)])
+def test_codes_of_many_tokens_feature_major(tsvd, B, N, dtype):
+    """As many tokens as take one launch whatever the features are: codes and scales as the formula has them (in 64 bits, on the GPU), over a buffer that held others, and a layer of them as from
+    token-major x."""
+    import torch
+    print(f"case many {B} {N} {dtype}", flush=True)
+    g = torch.Generator(device="cuda:0").manual_seed(B + N)
+    x = torch.randn((N, B), generator=g, device="cuda:0")
+    x[N - 1, ::3] *= 9                                # (the last feature has the largest magnitude of every third token)
+    x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    q = torch.full((B, tsvd.tsvd_int8_row_bytes(N)), 99, dtype=torch.int8, device="cuda:0")[:, :N]
+    q, s = tsvd.tsvd_int8_quantize(x, x_layout=tsvd.TSVD_FEATURE_MAJOR, codes=q)
+    a = x.double().abs().amax(0).clamp_min(SMALLEST)
+    assert torch.equal(s, (a / 127).float())
+    assert torch.equal(q, (x.double() * (127 / a).float().double()).round().to(torch.int8).t())
+    w, t, _ = layer(np.random.default_rng(N), 20, N)
+    h = packed(tsvd, w, t)
+    assert torch.equal(tsvd.tsvd_int8_forward(h, x, x_layout=tsvd.TSVD_FEATURE_MAJOR), tsvd.tsvd_int8_forward(h, x.t().contiguous(), x_layout=tsvd.TSVD_TOKEN_MAJOR))
+    tsvd.tsvd_int8_free(h)

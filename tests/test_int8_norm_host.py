@@ -93,3 +93,16 @@ def test_packing_needs_a_device():
     buf = (ctypes.c_char * 4096)()
     p = ctypes.addressof(buf)
     assert tsvd.load_library().tsvd_int8_pack(p, 32, p, 4, 32, None, 0, None, ctypes.byref(out)) == 4 and out.value is None
+
+
+@pytest.mark.parametrize("x_dtype", [0, 1])
+def test_codes_of_feature_major_activations_take_every_feature(x_dtype):
+    """One launch holds all features in registers or reads x twice; else there are two launches, and they need scratch.  On both sides of every border of the rules."""
+    tokens = sorted({b + d for b in (8, 16, 64, 512, 1024, 4096, 32704, 32768, 1 << 20, (1 << 24) - 1) for d in (-1, 0, 1)} | {1, 2})
+    features = sorted({n + d for n in (64, 512, 1024, 2048, 4096, 8192, 16384, (1 << 17) - 2) for d in (-1, 0, 1)} | {1, 4100, 9216, 14381})
+    for B in tokens:
+        for N in features:
+            holds = tsvd.tsvd_tuning_int8_columns(B, N, x_dtype)
+            assert (holds == -1) == (tsvd.tsvd_int8_quantize_workspace_bytes(B, N, tsvd.TSVD_FEATURE_MAJOR) > 0), (B, N)
+            assert holds in (-1, 0) or holds >= N, (B, N, holds)
+    assert tsvd.tsvd_tuning_int8_columns(0, 5, x_dtype) == tsvd.tsvd_tuning_int8_columns(5, 1 << 17, x_dtype) == -1

@@ -444,20 +444,20 @@ PyObject* py_group_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         need_args(n, CODES ? 10 : 11, CODES ? "group_norm_int8" : "group_norm");
         PyObject *const workspace = a[CODES ? 8 : 9], *const stream_arg = a[CODES ? 9 : 10];
         const at::Tensor& x = tensor_of(a[0], "x");
-        static const char* const text = "x must be a GPU tensor [rows,C], [images,positions,C] or [images,H,W,C] with unit inner stride and one pitch from a position to the next";
+        static const char* const text = "x must be [rows,C], [images,positions,C] or [images,H,W,C] with unit inner stride and a pitch of C or more, the same everywhere, from a position to the next";
         const int64_t d = x.dim();
-        if (!x.is_cuda() || d < 2 || d > 4 || x.numel() == 0 || (x.size(d - 1) > 1 && x.stride(d - 1) != 1)) raise(PyExc_ValueError, text);
-        const c10::DeviceGuard device(x.device());
+        if (d < 2 || d > 4 || x.numel() == 0 || (x.size(d - 1) > 1 && x.stride(d - 1) != 1)) raise(PyExc_ValueError, text);
         const int64_t C = x.size(d - 1), images = x.size(0), P = x.numel() / (images * C);
-        int64_t ldx = 0, before = 1;                                   // the pitch that every dimension longer than one has to agree with
+        // the innermost dimension longer than one has the pitch, and those around it follow (a stride of 0, of a broadcast view, is no pitch)
+        int64_t ldx = C, before = 1;
         for (int64_t k = d - 2; k >= 0; --k) {
-            if (x.size(k) > 1) {
-                if (ldx == 0 && x.stride(k) % before == 0) ldx = x.stride(k) / before;
-                if (x.stride(k) != ldx * before) raise(PyExc_ValueError, text);
-            }
+            if (x.size(k) == 1) continue;
+            if (before == 1) ldx = x.stride(k);
+            if (ldx < C || x.stride(k) != ldx * before) raise(PyExc_ValueError, text);
             before *= x.size(k);
         }
-        if (ldx == 0) ldx = C;
+        if (!x.is_cuda()) raise(PyExc_ValueError, "x must live on the GPU");
+        const c10::DeviceGuard device(x.device());
         const tsvd_dtype xd = dtype_code(x);
         const int64_t groups = integer(a[1]);
         const float *gamma = floats_of(a[2], C, x, "gamma must be a contiguous float32 GPU tensor [C] on x's device"),

@@ -106,3 +106,24 @@ def test_codes_of_feature_major_activations_take_every_feature(x_dtype):
             assert (holds == -1) == (tsvd.tsvd_int8_quantize_workspace_bytes(B, N, tsvd.TSVD_FEATURE_MAJOR) > 0), (B, N)
             assert holds in (-1, 0) or holds >= N, (B, N, holds)
     assert tsvd.tsvd_tuning_int8_columns(0, 5, x_dtype) == tsvd.tsvd_tuning_int8_columns(5, 1 << 17, x_dtype) == -1
+
+
+def test_norm_refuses_views_whose_positions_have_no_pitch():
+    """Positions that share their memory (a broadcast view), overlap or stand at different distances are refused by their strides, before anything asks where they are; every pitch of
+    C or more passes on to the next check, which on the CPU is the one for the device."""
+    import torch
+    row, images = torch.zeros(1, 24), torch.zeros(2, 1, 24)
+    wide = torch.zeros(2, 3, 4, 40)[..., :24]
+    refused = (row.expand(5, 24), row[None].expand(1, 5, 24), row[None].expand(2, 1, 24), row[None].expand(2, 5, 24), images.expand(2, 5, 24),
+               torch.zeros(2, 1, 120)[:, :, :24].expand(2, 5, 24), torch.zeros(5, 1, 24).transpose(0, 1).expand(2, 5, 24), row[None, None].expand(2, 3, 4, 24),
+               torch.zeros(2, 1, 1, 24).expand(2, 1, 4, 24), torch.zeros(100).as_strided((4, 24), (20, 1)), torch.zeros(300).as_strided((2, 3, 24), (144, 24, 1)),
+               torch.zeros(2, 5, 24).transpose(0, 1), torch.zeros(5, 24, 2)[:, :, 0],
+               wide[:, :1])                              # (rows 40 apart, images 480 where four rows take 160)
+    for x in refused:
+        for call in (tsvd.tsvd_group_norm, tsvd.tsvd_group_norm_int8):
+            with pytest.raises(ValueError, match="a pitch of C or more"):
+                call(x, 4)
+    for x in (row, images, wide, wide[0], wide[:, :, :1, :][:, :1], wide.flatten(0, 2), torch.zeros(1, 15, 24)[:, ::3], torch.zeros(2, 1, 100)[:, :, :24].transpose(0, 1)):
+        for call in (tsvd.tsvd_group_norm, tsvd.tsvd_group_norm_int8):
+            with pytest.raises(ValueError, match="live on the GPU"):
+                call(x, 4)

@@ -23,6 +23,7 @@ namespace {
 
 PyObject* error_class = nullptr;       // TsvdError(status, where)
 PyObject* raw_stream = nullptr;        // device index -> hipStream_t of torch's current stream, as an int
+PyObject *handle_class = nullptr, *int8_handle_class = nullptr;       // Handle, Int8Handle
 PyObject *name_ptr, *name_M, *name_N;
 
 struct failed {};                      // a Python error is set
@@ -41,13 +42,25 @@ int64_t attr_int(PyObject* o, PyObject* name) {
     return r;
 }
 
-struct handle_view {
-    const tsvd_handle* ptr;            // null after tsvd_free: the library rejects it
+template <typename T>
+struct view_of {
+    const T* ptr;                      // null after the handle is freed: the library rejects it
     int64_t M, N;
 };
-handle_view handle_of(PyObject* h) {
-    return {reinterpret_cast<const tsvd_handle*>((uintptr_t)attr_int(h, name_ptr)), attr_int(h, name_M), attr_int(h, name_N)};
+// (the class is checked: a handle of the other kind has the same attributes, and another struct behind them)
+template <typename T>
+view_of<T> view_handle(PyObject* h, PyObject* cls) {
+    PyTypeObject* type = reinterpret_cast<PyTypeObject*>(cls);
+    if (!PyObject_TypeCheck(h, type)) {
+        PyErr_Format(PyExc_TypeError, "h must be a %s, not %.100s", type->tp_name, Py_TYPE(h)->tp_name);
+        throw failed();
+    }
+    return {reinterpret_cast<const T*>((uintptr_t)attr_int(h, name_ptr)), attr_int(h, name_M), attr_int(h, name_N)};
 }
+typedef view_of<tsvd_handle> handle_view;
+typedef view_of<tsvd_int8_handle> int8_handle_view;
+handle_view handle_of(PyObject* h) { return view_handle<tsvd_handle>(h, handle_class); }
+int8_handle_view int8_handle_of(PyObject* h) { return view_handle<tsvd_int8_handle>(h, int8_handle_class); }
 
 const at::Tensor& tensor_of(PyObject* o, const char* what) {
     if (!THPVariable_Check(o)) {
@@ -279,7 +292,6 @@ PyObject* py_conv2d(PyObject*, PyObject* const* a, Py_ssize_t n) {
 void same_device(const at::Tensor& t, const at::Tensor& x, const char* text) {
     if (t.device() != x.device()) raise(PyExc_ValueError, text);
 }
-const tsvd_int8_handle* int8_handle_of(const handle_view& h) { return reinterpret_cast<const tsvd_int8_handle*>(h.ptr); }
 // Results and workspaces made here belong to torch's current stream: work on another one needs the caller's own.
 void need_own(PyObject* given, PyObject* stream, const char* text) {
     if (given == Py_None && stream != Py_None) raise(PyExc_ValueError, text);
@@ -369,7 +381,7 @@ PyObject* py_int8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* py_int8_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         need_args(n, 9, "int8_layer");
-        const handle_view h = handle_of(a[0]);
+        const int8_handle_view h = int8_handle_of(a[0]);
         const at::Tensor& x = tensor_of(a[1], "x");
         if (!x.is_cuda() || x.dim() != 2 || x.stride(1) != 1) raise(PyExc_ValueError, "x must be a 2-d GPU tensor with unit inner stride");
         const c10::DeviceGuard device(x.device());
@@ -386,7 +398,7 @@ PyObject* py_int8_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor& yt = THPVariable_Unpack(y.p);
         same_device(yt, x, "y must live on x's device");
         const float* bias = floats_of(a[3], h.M, x, "bias must be a contiguous float32 GPU tensor [M] on x's device");
-        const size_t need = tsvd_int8_workspace_bytes(int8_handle_of(h), B, xd, xl);
+        const size_t need = tsvd_int8_workspace_bytes(h.ptr, B, xd, xl);
         if (need) need_own(a[7], a[8], "work on a stream of your own needs a workspace of your own");
         at::Tensor made;
         const workspace_view ws = scratch_of(a[7], need, x, &made);
@@ -396,7 +408,7 @@ PyObject* py_int8_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t ldy = row_pitch(yt);
         tsvd_status st;
         Py_BEGIN_ALLOW_THREADS
-        st = tsvd_int8_forward(int8_handle_of(h), xp, xd, xl, B, ldx, bias, yp, (tsvd_dtype)yd, yl, ldy, ws.ptr, ws.bytes, stream);
+        st = tsvd_int8_forward(h.ptr, xp, xd, xl, B, ldx, bias, yp, (tsvd_dtype)yd, yl, ldy, ws.ptr, ws.bytes, stream);
         Py_END_ALLOW_THREADS
         check(st, "tsvd_int8_forward");
         return y.release();
@@ -407,7 +419,7 @@ PyObject* py_int8_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* py_int8_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         need_args(n, 8, "int8_product");
-        const handle_view h = handle_of(a[0]);
+        const int8_handle_view h = int8_handle_of(a[0]);
         const codes_view c = codes_of(a[1]);
         const at::Tensor& q = THPVariable_Unpack(a[1]);
         const c10::DeviceGuard device(q.device());
@@ -429,7 +441,7 @@ PyObject* py_int8_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t ldy = row_pitch(yt);
         tsvd_status st;
         Py_BEGIN_ALLOW_THREADS
-        st = tsvd_int8_product(int8_handle_of(h), c.ptr, c.ldq, scales, c.B, bias, yp, (tsvd_dtype)yd, yl, ldy, stream);
+        st = tsvd_int8_product(h.ptr, c.ptr, c.ldq, scales, c.B, bias, yp, (tsvd_dtype)yd, yl, ldy, stream);
         Py_END_ALLOW_THREADS
         check(st, "tsvd_int8_product");
         return y.release();
@@ -515,14 +527,17 @@ PyObject* py_group_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// setup(error class, raw stream lookup)
+// setup(error class, raw stream lookup, Handle, Int8Handle)
 PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
-        need_args(n, 2, "setup");
-        Py_XDECREF(error_class);
-        Py_XDECREF(raw_stream);
-        error_class = Py_NewRef(a[0]);
-        raw_stream = Py_NewRef(a[1]);
+        need_args(n, 4, "setup");
+        if (!PyType_Check(a[2]) || !PyType_Check(a[3])) raise(PyExc_TypeError, "setup takes the classes of the handles");
+        PyObject** const kept[] = {&error_class, &raw_stream, &handle_class, &int8_handle_class};
+        for (int i = 0; i < 4; ++i) {
+            PyObject* before = *kept[i];
+            *kept[i] = Py_NewRef(a[i]);
+            Py_XDECREF(before);
+        }
         Py_RETURN_NONE;
     });
 }

@@ -124,7 +124,7 @@ def _load_binding():
     except ImportError as e:
         raise RuntimeError("the native binding _tsvd_torch.so is missing or does not load: build it with "
                            "`python -m paper_2308_07641_amd.build` (or __graft_entry__.build())") from e
-    _tsvd_torch.setup(TsvdError, torch._C._cuda_getCurrentRawStream)
+    _tsvd_torch.setup(TsvdError, torch._C._cuda_getCurrentRawStream, Handle, Int8Handle)
     _binding = _tsvd_torch
     return _binding
 
@@ -211,6 +211,13 @@ class Handle:
             pass
 
 
+def _ptr(h, kind):
+    """The pointer of a handle of this kind (None once it is freed): the two kinds have nothing in common behind it."""
+    if not isinstance(h, kind):
+        raise TypeError(f"h must be a {kind.__name__}, not {type(h).__name__}")
+    return h.ptr
+
+
 def tsvd_pack(U, S, V, dev_buf=None) -> Handle:
     """Packs and uploads to the current HIP device.  dev_buf: optional torch uint8 CUDA tensor."""
     U, S, V = _weights(U, S, V)
@@ -226,16 +233,17 @@ def tsvd_pack(U, S, V, dev_buf=None) -> Handle:
 
 
 def tsvd_unpack(h: Handle):
+    ptr = _ptr(h, Handle)
     U = np.empty((h.M, h.K), dtype=np.int8)
     S = np.empty(h.K, dtype=np.float32)
     V = np.empty((h.K, h.N), dtype=np.int8)
-    _check(load_library().tsvd_unpack(h.ptr, U.ctypes.data, S.ctypes.data, V.ctypes.data), "tsvd_unpack")
+    _check(load_library().tsvd_unpack(ptr, U.ctypes.data, S.ctypes.data, V.ctypes.data), "tsvd_unpack")
     return U, S, V
 
 
 def tsvd_info(h: Handle) -> dict:
     vals = [_i64() for _ in range(5)]
-    _check(load_library().tsvd_info(h.ptr, *[ctypes.byref(v) for v in vals]), "tsvd_info")
+    _check(load_library().tsvd_info(_ptr(h, Handle), *[ctypes.byref(v) for v in vals]), "tsvd_info")
     return dict(zip(("M", "K", "N", "nnzU", "nnzV"), (v.value for v in vals)))
 
 
@@ -249,7 +257,7 @@ def _dtype_code(t) -> int:
 
 
 def tsvd_workspace_bytes(h: Handle, B: int, x_dtype: int) -> int:
-    return int(load_library().tsvd_workspace_bytes(h.ptr, B, x_dtype))
+    return int(load_library().tsvd_workspace_bytes(_ptr(h, Handle), B, x_dtype))
 
 
 def tsvd_forward(h: Handle, x, y=None, workspace=None, stream=None):
@@ -262,7 +270,7 @@ def tsvd_forward(h: Handle, x, y=None, workspace=None, stream=None):
 
 
 def tsvd_workspace_bytes_ex(h: Handle, B: int, x_dtype: int, x_layout: int) -> int:
-    return int(load_library().tsvd_workspace_bytes_ex(h.ptr, B, x_dtype, x_layout))
+    return int(load_library().tsvd_workspace_bytes_ex(_ptr(h, Handle), B, x_dtype, x_layout))
 
 
 def tsvd_forward_ex(h: Handle, x, x_layout=TSVD_FEATURE_MAJOR, bias=None, y=None, y_dtype=TSVD_F32, workspace=None,
@@ -303,6 +311,7 @@ def tsvd_tuning_reset() -> None:
 def tsvd_tuning_forward_stages(h: Handle, x, y, stage_mask: int, workspace=None, stream=None):
     """tsvd_forward restricted to the kernels in stage_mask (1 column maxima, 2 stage V, 4 stage U)."""
     import torch
+    ptr = _ptr(h, Handle)
     x2 = x if x.dim() == 2 else x.unsqueeze(1)
     B = x2.shape[1]
     ldx = x2.stride(0) if x2.shape[0] > 1 else max(B, x2.stride(0))
@@ -312,7 +321,7 @@ def tsvd_tuning_forward_stages(h: Handle, x, y, stage_mask: int, workspace=None,
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     if stream is None:
         stream = torch.cuda.current_stream(x.device).cuda_stream
-    _check(load_library().tsvd_tuning_forward_stages(h.ptr, x2.data_ptr(), _dtype_code(x2), TSVD_FEATURE_MAJOR, B, ldx, None,
+    _check(load_library().tsvd_tuning_forward_stages(ptr, x2.data_ptr(), _dtype_code(x2), TSVD_FEATURE_MAJOR, B, ldx, None,
                                                      y.data_ptr(), TSVD_F32, ldy, ws_ptr, ws_bytes, stream, int(stage_mask)),
            "tsvd_tuning_forward_stages")
     return y
@@ -320,25 +329,25 @@ def tsvd_tuning_forward_stages(h: Handle, x, y, stage_mask: int, workspace=None,
 
 def tsvd_tuning_tile_shapes(h: Handle, B: int):
     sv, su = ctypes.c_int(-1), ctypes.c_int(-1)
-    if load_library().tsvd_tuning_tile_shapes(h.ptr, B, ctypes.byref(sv), ctypes.byref(su)) != 0:
+    if load_library().tsvd_tuning_tile_shapes(_ptr(h, Handle), B, ctypes.byref(sv), ctypes.byref(su)) != 0:
         raise ValueError("tsvd_tuning_tile_shapes")
     return sv.value, su.value
 
 
 def tsvd_tuning_one_launch(h: Handle, B: int) -> bool:
-    return bool(load_library().tsvd_tuning_one_launch(h.ptr, B))
+    return bool(load_library().tsvd_tuning_one_launch(_ptr(h, Handle), B))
 
 
 def tsvd_tuning_split_tiles(h: Handle, B: int, x_dtype: int):
     v, u = ctypes.c_int(0), ctypes.c_int(0)
-    if load_library().tsvd_tuning_split_tiles(h.ptr, B, x_dtype, ctypes.byref(v), ctypes.byref(u)) != 0:
+    if load_library().tsvd_tuning_split_tiles(_ptr(h, Handle), B, x_dtype, ctypes.byref(v), ctypes.byref(u)) != 0:
         raise ValueError("tsvd_tuning_split_tiles: the call takes none of the plane path's tiles")
     return v.value, u.value
 
 
 def tsvd_tuning_tiles_by_xcd(h: Handle, B: int, x_dtype: int):
     v, u = ctypes.c_int(0), ctypes.c_int(0)
-    if load_library().tsvd_tuning_tiles_by_xcd(h.ptr, B, x_dtype, ctypes.byref(v), ctypes.byref(u)) != 0:
+    if load_library().tsvd_tuning_tiles_by_xcd(_ptr(h, Handle), B, x_dtype, ctypes.byref(v), ctypes.byref(u)) != 0:
         raise ValueError("tsvd_tuning_tiles_by_xcd: the call takes no split tiles")
     return bool(v.value), bool(u.value)
 
@@ -364,7 +373,7 @@ def tsvd_tuning_int8_columns(B: int, N: int, x_dtype: int) -> int:
 
 def tsvd_tuning_read_clocks(h: Handle, workgroups: int) -> np.ndarray:
     out = np.zeros((workgroups, 16), dtype=np.int64)
-    if load_library().tsvd_tuning_read_clocks(h.ptr, out.ctypes.data, workgroups) != 0:
+    if load_library().tsvd_tuning_read_clocks(_ptr(h, Handle), out.ctypes.data, workgroups) != 0:
         raise ValueError("tsvd_tuning_read_clocks: the handle was not packed with TSVD_CLOCKS = 1")
     return out
 
@@ -530,12 +539,12 @@ def tsvd_int8_pack(codes, scales, dev_buf=None, stream=None) -> Int8Handle:
 
 def tsvd_int8_info(h: Int8Handle) -> dict:
     vals = [_i64() for _ in range(2)]
-    _check(load_library().tsvd_int8_info(h.ptr, *[ctypes.byref(v) for v in vals]), "tsvd_int8_info")
+    _check(load_library().tsvd_int8_info(_ptr(h, Int8Handle), *[ctypes.byref(v) for v in vals]), "tsvd_int8_info")
     return dict(zip(("M", "N"), (v.value for v in vals)))
 
 
 def tsvd_int8_workspace_bytes(h: Int8Handle, B: int, x_dtype: int, x_layout: int) -> int:
-    return int(load_library().tsvd_int8_workspace_bytes(h.ptr, B, x_dtype, x_layout))
+    return int(load_library().tsvd_int8_workspace_bytes(_ptr(h, Int8Handle), B, x_dtype, x_layout))
 
 
 def tsvd_int8_forward(h: Int8Handle, x, x_layout=TSVD_FEATURE_MAJOR, bias=None, y=None, y_dtype=TSVD_F32, y_layout=TSVD_FEATURE_MAJOR,
@@ -553,7 +562,7 @@ def tsvd_int8_product(h: Int8Handle, codes, scales, bias=None, y=None, y_dtype=T
 
 
 def tsvd_int8_free(h: Int8Handle) -> None:
-    if h is not None and getattr(h, "ptr", None):
+    if h is not None and _ptr(h, Int8Handle):
         load_library().tsvd_int8_free(h.ptr)
         h.ptr = None
 
@@ -580,6 +589,6 @@ def tsvd_group_norm_int8(x, groups: int, gamma=None, beta=None, eps: float = 1e-
 
 
 def tsvd_free(h: Handle) -> None:
-    if h is not None and getattr(h, "ptr", None):
+    if h is not None and _ptr(h, Handle):
         load_library().tsvd_free(h.ptr)
         h.ptr = None

@@ -127,3 +127,42 @@ def test_norm_refuses_views_whose_positions_have_no_pitch():
         for call in (tsvd.tsvd_group_norm, tsvd.tsvd_group_norm_int8):
             with pytest.raises(ValueError, match="live on the GPU"):
                 call(x, 4)
+
+
+def test_a_handle_of_the_other_kind_is_a_type_error():
+    """Ternary and 8-bit handles of one layer have the same sizes but nothing else in common: every function takes its own kind only, whatever else is wrong with the call."""
+    import torch
+    ternary, int8 = tsvd.Handle(None, 8, 4, 16), tsvd.Int8Handle(None, 8, 16)
+    x, y, codes, scales = torch.zeros(16, 2), torch.zeros(8, 2), torch.zeros((2, 16), dtype=torch.int8), torch.zeros(2)
+
+    class Looks:
+        ptr, M, K, N = None, 8, 4, 16
+
+    for h in (int8, Looks(), None, 5):
+        for call in (lambda: tsvd.tsvd_forward(h, x), lambda: tsvd.tsvd_forward_ex(h, x), lambda: tsvd.tsvd_forward_io(h, x), lambda: tsvd.tsvd_forward_noalloc(h, x, y),
+                     lambda: tsvd.tsvd_conv2d_forward(h, 0, 16, 8, 1, 1, x.view(16, 1, 2, 1)), lambda: tsvd.tsvd_unpack(h), lambda: tsvd.tsvd_info(h),
+                     lambda: tsvd.tsvd_workspace_bytes(h, 2, 0), lambda: tsvd.tsvd_workspace_bytes_ex(h, 2, 0, 0), lambda: tsvd.tsvd_tuning_forward_stages(h, x, y, 7),
+                     lambda: tsvd.tsvd_tuning_tile_shapes(h, 2), lambda: tsvd.tsvd_tuning_one_launch(h, 2), lambda: tsvd.tsvd_tuning_split_tiles(h, 2, 0),
+                     lambda: tsvd.tsvd_tuning_tiles_by_xcd(h, 2, 0), lambda: tsvd.tsvd_tuning_read_clocks(h, 1)):
+            with pytest.raises(TypeError, match="Handle"):
+                call()
+    for h in (ternary, Looks(), None, 5):
+        for call in (lambda: tsvd.tsvd_int8_forward(h, x), lambda: tsvd.tsvd_int8_product(h, codes, scales), lambda: tsvd.tsvd_int8_info(h),
+                     lambda: tsvd.tsvd_int8_workspace_bytes(h, 2, 0, 0)):
+            with pytest.raises(TypeError, match="Int8Handle"):
+                call()
+    for free, h in ((tsvd.tsvd_free, int8), (tsvd.tsvd_int8_free, ternary), (tsvd.tsvd_free, Looks()), (tsvd.tsvd_int8_free, 5)):
+        with pytest.raises(TypeError):
+            free(h)
+    for free, h in ((tsvd.tsvd_free, None), (tsvd.tsvd_int8_free, None), (tsvd.tsvd_free, ternary), (tsvd.tsvd_int8_free, int8)):
+        free(h)
+    # one's own kind, released: the library refuses it
+    for call in (lambda: tsvd.tsvd_info(ternary), lambda: tsvd.tsvd_int8_info(int8)):
+        with pytest.raises(tsvd.TsvdError):
+            call()
+
+    class Own(tsvd.Int8Handle):
+        pass
+
+    with pytest.raises(tsvd.TsvdError):
+        tsvd.tsvd_int8_info(Own(None, 8, 16))

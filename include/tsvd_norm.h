@@ -6,8 +6,9 @@
  * channels in each group.  For every image and group, over its positions and channels:
  *   mu = mean of x,  v = mean of (x - mu)^2,  h = (x - mu) / sqrt(v + eps) gamma_c + beta_c,  y = act(h)
  * groups = 1 and positions = 1 is the layer norm of `images` tokens.
- * Mean and variance are taken in fp32, the variance from the deviations from a mean (never as a difference of squares), and
- * everything up to act(h) in fp32.  A group that holds an infinity or NaN gives NaN in its own outputs and no others.
+ * Mean and variance are taken in fp32, from deviations: of values from one of the values themselves, of pieces of a group (joined in
+ * fp64) from the mean of one of them, so that no square of a mean enters; everything up to act(h) is fp32.  A group that holds an
+ * infinity or NaN gives NaN in its own outputs and no others.
  * Results do not depend on what runs beside the call: the sums have a fixed order.
  *
  * Status codes, streams and ownership are those of tsvd.h: calls enqueue on `stream` and return without synchronising; on failure

@@ -3,7 +3,8 @@
 // Bound by memory: x once and y once where a workgroup can hold what it normalises, else x twice.  A thread keeps eight neighbouring channels and walks along the
 // positions: sums of x - k and (x - k)^2 for each channel, k being the first value that it meets.  As k is one of the values, the deviations that cancel are
 // part of the result: the sum of squares about the thread's own mean is right to the number of its values times 2^-24, whatever the values are.  Threads, and pieces of an
-// image, are then joined as counts, sums and sums of squares in fp64, where what cancels is 2^-53 of the mean's square.  Every sum has a fixed order.
+// image, are then joined in fp64 the same way, as counts, sums and sums of squares about the mean of the first of them.  Every sum has a fixed order.  What is left of a large mean is the
+// rounding of the pieces' means to fp32.
 //
 // Forms: rows (one position and one group: a row in registers), one launch (a workgroup has all positions of an image for some groups, or whole images: codes), and two launches
 // (statistics of pieces; y or codes, every workgroup joining the pieces that it needs; x comes a second time, from the memory-side cache where it fits).
@@ -241,14 +242,23 @@ __device__ __forceinline__ T lanes_sum(T v, int log) {
     if (log > 5) v += norm_xor<32>(v);
     return v;
 }
-// Numbers, sums and sums of squares of 2^log lanes -> mean, and the sum of squared deviations or 1 / sqrt(v + eps).
+// Pieces of one group, about the mean k of the first of them (which has values): their number, sum, and sum of squares.
+struct norm_join {
+    double k, n = 0, sum = 0, sq = 0;
+    __device__ __forceinline__ explicit norm_join(float first) : k(first) {}
+    __device__ __forceinline__ void add(float mean, float m2, float count) {
+        const double d = mean - k, nd = count * d;
+        n += count, sum += nd, sq += m2 + nd * d;
+    }
+};
+// Those of 2^log lanes -> mean, and the sum of squared deviations or 1 / sqrt(v + eps).
 template <bool FINAL>
-__device__ __forceinline__ void store_joined(double n, double sum, double sq, int log, float eps, bool mine, float* mean, float* m2) {
-    n = lanes_sum(n, log), sum = lanes_sum(sum, log), sq = lanes_sum(sq, log);
+__device__ __forceinline__ void store_joined(const norm_join& of, int log, float eps, bool mine, float* mean, float* m2) {
+    const double n = lanes_sum(of.n, log), sum = lanes_sum(of.sum, log), sq = lanes_sum(of.sq, log);
     if (!mine) return;
-    // (n is a whole number: its reciprocal in fp32, corrected once, is right to 2^-46)
-    const double r0 = __builtin_amdgcn_rcpf((float)n), inv = r0 * (2.0 - n * r0), mu = sum * inv, dev = sq - sum * mu;
-    *mean = (float)mu;
+    // (n is a whole number: its reciprocal in fp32, corrected once, is right to 2^-45, of a mean that is as large as the deviations)
+    const double r0 = __builtin_amdgcn_rcpf((float)n), inv = r0 * (2.0 - n * r0), off = sum * inv, dev = sq - sum * off;
+    *mean = (float)(of.k + off);
     if constexpr (FINAL) {
         const float v = (float)(dev * inv);
         *m2 = __builtin_amdgcn_rsqf((v < 0.f ? 0.f : v) + eps);       // (a variance that is no number stays none)
@@ -256,8 +266,7 @@ __device__ __forceinline__ void store_joined(double n, double sum, double sq, in
         *m2 = (float)dev;
     }
 }
-// Means and sums of squared deviations of the workgroup's groups from its threads' sums.  The pieces are added up as sums of values and squares in 64 bits: what
-// cancels there is 2^-53 of the mean's square.
+// Means and sums of squared deviations of the workgroup's groups from its threads' sums.
 // (FINAL: 1 / sqrt(v + eps) in the place of the sum of squares)
 template <int T, bool FINAL>
 __device__ __forceinline__ void join_threads(const norm_lds& l, const norm_sums& s, int at, int r, int cvec, int R, int nch, int ng, int cg, float eps) {
@@ -292,19 +301,22 @@ __device__ __forceinline__ void join_threads(const norm_lds& l, const norm_sums&
     __syncthreads();
     const int log = lanes_log2(ng, T), L = 1 << log, lane = tid & (L - 1);
     for (int g = tid >> log; g < ((ng + (T >> log) - 1) & -(T >> log)); g += T >> log) {       // (whole wavefronts)
-        double n = 0, sum = 0, sq = 0;
+        norm_join join(0.f);
         if (g < ng) {
             const int a0 = (g * cg) >> 3, nv = ((g * cg + cg - 1) >> 3) - a0 + 1, step_r = quotient(L, nv), step_k = L - step_r * nv;
             int row = quotient(lane, nv), k = lane - row * nv;
             const norm_piece* from = l.piece + a0 + g;
+            // (the mean of the first piece is read behind the lane's own first one: one wait for both)
+            norm_piece q = from[min(row, R - 1) * (cvec + ng) + k];
+            join = norm_join(from->mean);
             while (row < R) {
-                const norm_piece q = from[row * (cvec + ng) + k];
-                n += q.n, sum += (double)q.n * q.mean, sq += q.m2 + (double)q.n * q.mean * q.mean;
+                join.add(q.mean, q.m2, q.n);
                 row += step_r, k += step_k;
                 if (k >= nv) k -= nv, ++row;
+                q = from[min(row, R - 1) * (cvec + ng) + k];
             }
         }
-        store_joined<FINAL>(n, sum, sq, log, eps, g < ng && lane == 0, l.mean + g, l.m2 + g);
+        store_joined<FINAL>(join, log, eps, g < ng && lane == 0, l.mean + g, l.m2 + g);
     }
     __syncthreads();
 }
@@ -526,15 +538,22 @@ __device__ __forceinline__ void join_parts(const norm_args& p, long long image, 
     const int tid = threadIdx.x, chunks = (int)p.chunks, log = lanes_log2(ng, T), L = 1 << log, lane = tid & (L - 1);
     for (int g = tid >> log; g < ((ng + (T >> log) - 1) & -(T >> log)); g += T >> log) {
         const float4* a = p.parts + (image * p.G + g0 + min(g, ng - 1)) * p.chunks;
-        double n = 0, sum = 0, sq = 0;
-        auto add = [&](const float4& q) { n += q.z, sum += (double)q.z * q.x, sq += q.y + (double)q.z * q.x * q.x; };
-        int c = lane;
-        for (; c + 3 * L < chunks; c += 4 * L) {
-            const float4 q0 = a[c], q1 = a[c + L], q2 = a[c + 2 * L], q3 = a[c + 3 * L];
-            add(q0), add(q1), add(q2), add(q3);
+        // (the mean of the first piece is asked for behind the lane's own first ones: one wait for all of them)
+        float4 q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i == 0 || i * L < chunks) q[i] = a[min(lane + i * L, chunks - 1)];
+        norm_join join(a[0].x);
+        for (int c = lane;;) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + i * L < chunks) join.add(q[i].x, q[i].y, q[i].z);
+            c += 4 * L;
+            if (c >= chunks) break;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = a[min(c + i * L, chunks - 1)];
         }
-        for (; c < chunks; c += L) add(a[c]);
-        store_joined<true>(n, sum, sq, log, p.eps, g < ng && lane == 0, mean + g, rstd + g);
+        store_joined<true>(join, log, p.eps, g < ng && lane == 0, mean + g, rstd + g);
     }
     __syncthreads();
 }

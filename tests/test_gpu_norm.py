@@ -132,6 +132,31 @@ def test_norm_to_codes(tsvd, images, P, C, G, dtype):
         assert np.all(np.abs(q * s[:, None] - want) <= 0.5 * s[:, None] * (1 + 1e-5) + tol + off[:, None])
 
 
+# rows, one launch (lanes of 64, 256, 512), pieces and codes of each
+FAR = [(3, 1, 512, 1), (600, 9, 64, 8), (1, 333, 8, 1), (2, 100, 64, 2), (2, 1999, 32, 4), (1, 10007, 8, 2), (2, 5003, 96, 3), (1, 1201, 256, 1), (2, 49, 1280, 4), (3, 7, 5000, 1)]
+
+
+@pytest.mark.parametrize("images,P,C,G", FAR)
+def test_means_far_from_zero(tsvd, images, P, C, G):
+    """Means 2^21 and 2^23 times the deviations: channels c - d, c + d in turn, all exact in fp32, and so are a thread's mean c and deviations d whatever it holds (whole vectors; means of
+    rows need c up to 2^17).  What is left: the squares of a thread (8 additions), the joined variance, 1 / sqrt and the product: 16 roundings of 2^-24 and one of 2^-23."""
+    import torch
+    for c, d in ((2.0 ** 17, 2.0 ** -4), (2.0 ** 20, 2.0 ** -3)):
+        if P == 1 and G == 1 and c > 2.0 ** 17:
+            continue
+        print(f"case far {images} {P} {C} {G} {c}", flush=True)
+        x = torch.full((images, P, C), c, device="cuda:0")
+        x[..., ::2] -= d
+        x[..., 1::2] += d
+        eps = np.float64(np.float32(1e-9))
+        want = d / np.sqrt(d * d + eps)
+        y = tsvd.tsvd_group_norm(x, G, eps=1e-9).double()
+        assert float((y[..., 1::2] - want).abs().max()) <= 18 * U * want and float((y[..., ::2] + want).abs().max()) <= 18 * U * want
+        q, s = tsvd.tsvd_group_norm_int8(x, G, eps=1e-9)
+        assert bool((q[:, 1::2] == 127).all()) and bool((q[:, ::2] == -127).all())
+        assert float((s.double() * 127 - want).abs().max()) <= 20 * U * want
+
+
 @pytest.mark.parametrize("images,P,C,G", [(2, 50, 64, 4), (3, 1, 512, 1), (1, 3000, 96, 32), (2, 600, 16, 2)])
 def test_a_value_that_is_no_number_stays_in_its_group(tsvd, images, P, C, G):
     import torch

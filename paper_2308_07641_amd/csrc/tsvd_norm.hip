@@ -6,7 +6,7 @@
 // image, are then joined in fp64 the same way, as counts, sums and sums of squares about the mean of the first of them.  Every sum has a fixed order.  What is left of a large mean is the
 // rounding of the pieces' means to fp32.
 //
-// Forms: rows (one position and one group: a row in registers), one launch (a workgroup has all positions of an image for some groups, or whole images: codes), and two launches
+// Forms: rows (one position and one group: a row in registers, its sums about its first value), one launch (a workgroup has all positions of an image for some groups, or whole images: codes), and two launches
 // (statistics of pieces; y or codes, every workgroup joining the pieces that it needs; x comes a second time, from the memory-side cache where it fits).
 //
 // Measured: 16 images of 16384 positions, 256 channels in 32 groups, bf16: statistics 40 us (3.3 TB/s), y 47 us (5.6 TB/s both ways); 8 of 1024 x 640 in one launch 11.8 us; one of
@@ -54,6 +54,9 @@ template <int J>
 __device__ __forceinline__ float norm_xor(float v) { return __uint_as_float(lane_xor32<J>(__float_as_uint(v))); }
 template <int J>
 __device__ __forceinline__ double norm_xor(double v) { return lane_xor<J>(v); }
+
+__device__ __forceinline__ float value_of(float x) { return x; }
+__device__ __forceinline__ float value_of(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
 // a / b for 0 <= a < 2^20, b >= 1: (a + 1/2) / b is 1 / (2 b) away from a whole number at least, more than the two roundings.  (A division of integers takes some forty
 // instructions, one of 64 bits hundreds, and everything here waits for them.)
@@ -784,8 +787,9 @@ norm_rows_kernel(norm_args p) {
         for (int k = 0; k < NV; ++k) ch[k].load(p, WHOLE ? 8 * min(t + k * T, C / 8 - 1) : min(8 * (t + k * T), C - 1), WHOLE ? 8 : max(1, min(8, C - 8 * (t + k * T))));
         const long long step = (long long)gridDim.x * ROWS;
         long long row = (long long)blockIdx.x * ROWS + threadIdx.x / T;
-        auto load = [&](int8_eight<X> (&v)[NV], long long at) {
+        auto load = [&](int8_eight<X> (&v)[NV], X& first, long long at) {
             const X* x = static_cast<const X*>(p.x) + min(at, p.images - 1) * p.ldx;
+            first = x[0];
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 if constexpr (WHOLE) v[k].load(x + 8 * min(t + k * T, C / 8 - 1));
@@ -793,19 +797,24 @@ norm_rows_kernel(norm_args p) {
             }
         };
         int8_eight<X> v[NV];
-        load(v, row);
+        X first;
+        load(v, first, row);
         for (; row < p.images; row += step) {
+            // values from the row's first one on: rows without deviation give beta, and a large mean costs nothing
             float f[NV][8], sum = 0.f;
+            const float from = value_of(first);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[k][e] = v[k].get(e);
-            load(v, row + step);
+                for (int e = 0; e < 8; ++e) f[k][e] = v[k].get(e) - from;
+            load(v, first, row + step);
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (!WHOLE || 8 * (t + k * T) < C)
+            for (int k = 0; k < NV; ++k) {
+                const int n = C - 8 * (t + k * T);
+                if (!WHOLE || n > 0)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum += f[k][e];              // (zeros behind the end)
+                    for (int e = 0; e < 8; ++e) sum += WHOLE || e < n ? f[k][e] : 0.f;
+            }
             const float mean = reduce(sum, 0) / (float)C;
             float m2 = 0.f;
 #pragma unroll

@@ -138,12 +138,10 @@ FAR = [(3, 1, 512, 1), (600, 9, 64, 8), (1, 333, 8, 1), (2, 100, 64, 2), (2, 199
 
 @pytest.mark.parametrize("images,P,C,G", FAR)
 def test_means_far_from_zero(tsvd, images, P, C, G):
-    """Means 2^21 and 2^23 times the deviations: channels c - d, c + d in turn, all exact in fp32, and so are a thread's mean c and deviations d whatever it holds (whole vectors; means of
-    rows need c up to 2^17).  What is left: the squares of a thread (8 additions), the joined variance, 1 / sqrt and the product: 16 roundings of 2^-24 and one of 2^-23."""
+    """Means 2^21 and 2^23 times the deviations: channels c - d, c + d in turn, all exact in fp32, and so are a thread's mean c and deviations d whatever it holds (whole vectors).
+    What is left: the squares of a thread (8 additions), the joined variance, 1 / sqrt and the product: 16 roundings of 2^-24 and one of 2^-23."""
     import torch
     for c, d in ((2.0 ** 17, 2.0 ** -4), (2.0 ** 20, 2.0 ** -3)):
-        if P == 1 and G == 1 and c > 2.0 ** 17:
-            continue
         print(f"case far {images} {P} {C} {G} {c}", flush=True)
         x = torch.full((images, P, C), c, device="cuda:0")
         x[..., ::2] -= d
@@ -155,6 +153,23 @@ def test_means_far_from_zero(tsvd, images, P, C, G):
         q, s = tsvd.tsvd_group_norm_int8(x, G, eps=1e-9)
         assert bool((q[:, 1::2] == 127).all()) and bool((q[:, ::2] == -127).all())
         assert float((s.double() * 127 - want).abs().max()) <= 20 * U * want
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("images,P,C,G", FAR + [(5, 1, 100, 1), (20, 1, 128, 1), (9, 1, 250, 1), (5, 1, 513, 1), (3, 1, 1001, 1), (3, 1, 2048, 1), (3, 1, 4095, 1), (2, 1, 8191, 1), (2, 1, 16384, 1)])
+def test_groups_without_deviation(tsvd, images, P, C, G, dtype):
+    """All values of a group alike: every deviation is exactly 0, whatever the value, and y is beta to the last bit."""
+    import torch
+    beta = torch.randn(C, device="cuda:0")
+    gamma = torch.randn(C, device="cuda:0")
+    for value in (100000.3, -0.7, 3.0e-5, 1.0e30):
+        print(f"case alike {images} {P} {C} {G} {dtype} {value}", flush=True)
+        x = torch.full((images, P, C), value, device="cuda:0", dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+        y = tsvd.tsvd_group_norm(x, G, gamma, beta, y_dtype=tsvd.TSVD_F32)
+        assert torch.equal(y, beta.expand(images, P, C))
+        q, s = tsvd.tsvd_group_norm_int8(x, G, gamma, beta)
+        codes, scale = tsvd.tsvd_int8_quantize(beta[None])
+        assert torch.equal(q, codes.expand(images * P, C)) and torch.equal(s, scale.expand(images * P))
 
 
 @pytest.mark.parametrize("images,P,C,G", [(2, 50, 64, 4), (3, 1, 512, 1), (1, 3000, 96, 32), (2, 600, 16, 2)])

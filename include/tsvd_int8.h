@@ -7,8 +7,8 @@
  *   a_b = max(max_n |x_bn|, 2^-100),  s_b = fl(a_b / 127),  r_b = fl(127 / a_b),  q_bn = the whole number nearest to x_bn r_b
  *   y_bm = (sum_n q_bn w_mn) s_b t_m + bias_m
  * fl rounds to fp32; the product x r is not rounded before the whole number is taken, ties go to the even one, and |q| <= 127.
- * The sum is an exact whole number (N below 2^17); the rest is fp32 arithmetic: y is within 2^-22 of |(sum) s t| + |bias| of what
- * the formula gives, then rounded to nearest even where y is bf16.  A token's result does not depend on the tokens beside it.
+ * The sum is an exact whole number (N below 2^17); the rest is fp32 arithmetic, ((sum) t) s + bias in this order: where (sum) t is zero
+ * or a normal number, y is within 2^-22 of |(sum) s t| + |bias| of what the formula gives, then rounded to nearest even where y is bf16.  A token's result does not depend on the tokens beside it.
  * A token that holds an infinity or NaN gets the scale NaN: its outputs are NaN, those of other tokens are as ever.  (All of the
  * 2^-100 floor: smaller tokens keep fewer bits, and a token of zeros has codes 0.)
  *
@@ -73,7 +73,8 @@ void tsvd_int8_free(tsvd_int8_handle* h);
  * y from codes that are there (several layers that read the same activations share them):
  *   y_dev : [M][B] with ldy >= B (TSVD_FEATURE_MAJOR) or [B][M] with ldy >= M (TSVD_TOKEN_MAJOR), of y_dtype, at any stride and element
  *           alignment.   bias_dev : device fp32 [M] or NULL.
- * TSVD_EINVAL as above, and where the current device is not the one of the handle; TSVD_EUNSUPPORTED: B > 2^24 or ldq > 2^22. */
+ * TSVD_EINVAL as above, and where the current device is not the one of the handle; TSVD_EUNSUPPORTED: B > 2^24, ldq > 2^22, or
+ * more than 2^23 tiles of 64 x 64 results or larger ones (M B above 2^35). */
 tsvd_status tsvd_int8_product(const tsvd_int8_handle* h, const int8_t* codes_dev, int64_t ldq, const float* scales_dev, int64_t B,
                               const float* bias_dev, void* y_dev, tsvd_dtype y_dtype, tsvd_layout y_layout, int64_t ldy, void* stream);
 

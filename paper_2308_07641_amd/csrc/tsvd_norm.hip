@@ -9,8 +9,8 @@
 // Forms: rows (one position and one group: a row in registers, its sums about its first value), one launch (a workgroup has all positions of an image for some groups, or whole images: codes), and two launches
 // (statistics of pieces; y or codes, every workgroup joining the pieces that it needs; x comes a second time, from the memory-side cache where it fits).
 //
-// Measured: 16 images of 16384 positions, 256 channels in 32 groups, bf16: statistics 40 us (3.3 TB/s), y 47 us (5.6 TB/s both ways); 8 of 1024 x 640 in one launch 11.8 us; one of
-// 64 x 320 5.0 us; 2048 rows of 4096 into codes 9 us (2.8 TB/s).
+// Measured: 16 images of 16384 positions, 256 channels in 32 groups, bf16: statistics 40 us (3.3 TB/s), y 47 us (5.6 TB/s both ways); 8 of 1024 x 640 in one launch 11.9 us; one of
+// 64 x 320 5.0 us; 2048 rows of 4096 into codes 9.1 us (2.8 TB/s; 7.9 back to back).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -873,6 +873,7 @@ size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
 unsigned grid_of(long long blocks) { return (unsigned)std::min<long long>(blocks, 1 << 20); }
 long long up(long long v, long long m) { return (v + m - 1) / m; }
 
+// (CUS: of a whole card, which the figures of the rules below were measured on.  Results do not depend on it.)
 constexpr int CUS = 256, VECS = 20, MAX_GROUPS = 4096;
 
 // Groups whose channels are whole vectors, where that takes 128 channels at most.
@@ -887,7 +888,7 @@ void cut(long long images, long long P, int C, int G, norm_args* a) {
     a->images = images, a->P = P, a->C = C, a->G = G, a->cg = C / G;
     a->gpb = std::min(G, VECS * 8 / a->cg);
     if (a->gpb <= 1 && a->cg > 64) {
-        a->gpb = 0;                                          // one group, by its vectors
+        a->gpb = 0;                                          // one group, by its vectors (16384 positions of 128 channels: 1024 pieces, 13.8 us where x and y alone take 2.5)
         a->nblk = G;
         const long long vecs = P * up(a->cg, 8);
         a->rows = (int)std::max<long long>(1, std::min<long long>(MAX_ROWS / 8, up(vecs * images * G, 1024 * 256)));
@@ -899,7 +900,8 @@ void cut(long long images, long long P, int C, int G, norm_args* a) {
     a->gpb = (int)(up(up(G, a->nblk), unit) * unit);
     a->nblk = (int)up(G, a->gpb);
     const int R = 256 / (int)up(a->gpb * a->cg, 8);
-    // up to 64 positions of a thread: about 512 workgroups, and at most 2048 pieces of an image, which workgroups of the next launch join
+    // up to 64 positions of a thread: about 512 workgroups, and about 2048 pieces (of all groups) of an image, which workgroups of the next launch join.  Larger images have more, as 64
+    // positions are the most: one of 1048576 positions, 128 channels in 32 groups has 1024 pieces for each group, which every workgroup reads for its own: 211 us, 161 without them
     const long long per = std::max<long long>(1, std::min<long long>(MAX_ROWS, std::max(up(images * a->nblk * P, 512 * R), up(P * G, 2048 * R))));
     a->rows = (int)std::min<long long>(per * R, P);
     a->chunks = up(P, a->rows);

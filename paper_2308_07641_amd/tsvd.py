@@ -576,7 +576,8 @@ def tsvd_group_norm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, ac
                     y_layout=TSVD_TOKEN_MAJOR, workspace=None, stream=None):
     """act(group norm) of x [images,positions,C] or [images,H,W,C] (channels last; [rows,C]: each row by itself), fp32 or bf16 on the GPU.
 
-    y has x's shape, or with y_layout=TSVD_FEATURE_MAJOR the channels first ([C,images,H,W], what tsvd_conv2d_forward reads); y_dtype: x's by default.
+    y has x's shape, or with y_layout=TSVD_FEATURE_MAJOR the channels first ([C,images,H,W], what tsvd_conv2d_forward reads); y_dtype: x's by default.  x may have any pitch from
+    one position to the next (C or more, not a broadcast view); a y of the caller's own is contiguous and shares no memory with x.
     """
     return (_binding or _load_binding()).group_norm(x, groups, gamma, beta, eps, act, y, _dtype_code(x) if y_dtype is None else y_dtype, y_layout,
                                                     workspace, stream)

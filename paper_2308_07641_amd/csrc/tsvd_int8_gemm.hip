@@ -10,7 +10,7 @@
 // next stage are read behind it while the last quarter is multiplied.
 //
 // What bounds it: with these operands the matrix unit alone, fed from registers, reaches 3.4e15 operations a second (5.0e15 with zeros: the clock follows the power), 36864 x 9216 at 2048
-// tokens runs at 2.35e15; half the compute units busy run at the higher clock, so a last round that is half empty costs little.
+// tokens runs at 2.2e15 to 2.35e15, by the card; half the compute units busy run at the higher clock, so a last round that is half empty costs little.
 #include "tsvd_int8.h"
 
 #include <algorithm>

@@ -11,7 +11,8 @@
 // MAKE: the codes are made here, by every workgroup for itself: each lane reads a part of the activations (ROWS: token-major, eight side by side; else those of its operand
 // places), the largest magnitudes of the tokens meet in LDS (the one barrier before the end), and the codes are there without a launch of their own.
 //
-// Measured, 16384 rows of 4096 features (64 MiB of weights): one token 11.7 us from its activations (5.7 TB/s), 16 tokens 11.9 us from codes and 13.4 from activations, 64 tokens 15.1 us.
+// Measured, 16384 rows of 4096 features (64 MiB of weights, which stay in the memory-side cache): one token 11.8 us from its activations (5.7 TB/s), 16 tokens 11.9 us from codes and 13.5 from
+// activations, 64 tokens 15.1 us.  Twelve such layers in turn, all weights from memory: one token 14.5 us (4.6 TB/s), 16 tokens 15.4 us.
 #include "tsvd_int8.h"
 
 #include <algorithm>
